@@ -283,6 +283,88 @@ int64_t cyc_attention_workspace(int64_t batch, int64_t N, int64_t M, int64_t d);
 int cyc_recurrence_attention_split(const void *Q, const void *K, const void *V, void *O, int64_t batch, int64_t N, int64_t M,
                                    int64_t d, void *workspace, int64_t workspace_bytes, void *stream);
 
+/* Attention with a causal mask, a sliding window and a few first keys that stay visible (sinks), with key heads that several query
+ * heads may share:
+ *     O_i. = sum_j exp(S_ij - lse_i) V_j. ,   S_ij = Q_i. K_j.^T / sqrt(d) ,   lse_i = log sum_j exp S_ij
+ * over the keys j that query i sees.  The N queries are the last of M positions: query i stands at p = i + M - N and sees
+ *     j <= p  and  (p - j < window  or  j < sinks).
+ * window 0: no window, plain causal attention.  A query with p < 0 (N > M) sees nothing: O_i. = 0, lse_i = -inf.
+ * Query head h reads key head h / (heads / kv_heads).
+ *
+ * Q, O: device, batch x heads x N x d bfloat16.  K, V: device, batch x kv_heads x M x d bfloat16.  lse: device, batch x heads x N
+ * fp32, dense, or NULL: not written.  strides (host, read before the call returns): the strides in elements of batch, head and row of
+ * Q, K, V and O, twelve numbers, or NULL: each dense in the order above.  Rows of d are contiguous; strides are
+ * multiples of 8 and pointers 16-byte aligned.  Inputs may have strides of 0 and overlap one another; O may not meet itself.
+ * d: 64 or 128.  N, M >= 0 and (heads / kv_heads) * N below 2^30, batch * heads below 2^24; window, sinks >= 0.
+ * Scores, maxima, sums and outputs are fp32 until O is rounded; the weights enter the product with V rounded to bfloat16 and
+ * their sum unrounded.  What lies in keys that a query does not see never reaches it, infinities and NaN included.
+ * workspace: as in cyc_recurrence_attention_split; cyc_attention_window_workspace says how many bytes the call wants (0: none;
+ * host only, also 0 for extents that the call refuses), and with less, or NULL, the keys are not split over workgroups.
+ * The same call with the same memory gives the same bits every time.  batch, heads or N == 0: CYC_OK, nothing done.
+ * Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE (also heads no multiple of kv_heads, misaligned pointers and
+ * strides, an O that meets itself), CYC_ERR_ALIAS (the memory from first to last element of O, lse or workspace overlaps that of
+ * another operand), CYC_ERR_LAUNCH. */
+int64_t cyc_attention_window_workspace(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d, int64_t window,
+                                       int64_t sinks);
+int cyc_recurrence_attention_window(const void *Q, const void *K, const void *V, void *O, void *lse, int64_t batch, int64_t heads,
+                                    int64_t kv_heads, int64_t N, int64_t M, int64_t d, const int64_t *strides, int64_t window,
+                                    int64_t sinks, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* Its gradient: with P_ij = exp(S_ij - lse_i) over visible keys, D_i = dO_i. O_i.^T and dS_ij = P_ij (dO_i. V_j.^T - D_i),
+ *     dQ_i. = sum_j dS_ij K_j. / sqrt(d) ,   dK_j. = sum_i dS_ij Q_i. / sqrt(d) ,   dV_j. = sum_i P_ij dO_i. ,
+ * dK and dV summed over the query heads that share the key head as well.  O and lse are what the forward call wrote for the same
+ * Q, K, V and mask; dO is like O; dQ, dK, dV (written) are like Q, K, V.  strides: of Q, K, V, O, dO, dQ, dK, dV, twenty-four
+ * numbers, or NULL.  P and dS enter the products rounded to bfloat16, all sums are fp32, the gradients are rounded once.  Queries
+ * that see nothing and keys that nobody sees get zeros.  No atomic adds: the same call gives the same bits every time.
+ * workspace: device, 16-byte aligned, not cleared, free again when the call's work on `stream` is done; the call needs
+ * cyc_attention_window_grad_workspace bytes and returns CYC_ERR_WORKSPACE with nothing enqueued if it gets less.
+ * Extents and errors otherwise: those of the forward call, kv_heads * M below 2^30; none of dQ, dK, dV may meet itself or overlap another operand. */
+int64_t cyc_attention_window_grad_workspace(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
+                                            int64_t window, int64_t sinks);
+int cyc_recurrence_attention_window_grad(const void *Q, const void *K, const void *V, const void *O, const void *lse, const void *dO,
+                                         void *dQ, void *dK, void *dV, int64_t batch, int64_t heads, int64_t kv_heads, int64_t N,
+                                         int64_t M, int64_t d, const int64_t *strides, int64_t window, int64_t sinks, void *workspace,
+                                         int64_t workspace_bytes, void *stream);
+
+/* A cache of keys and values in pages, and the sequences that a call works on.  Key j of sequence b is row j % page of page
+ * table[b * table_stride + j / page]; lengths[b] keys count, the call's new tokens among them, and the new tokens of sequence b, its
+ * last keys, are rows starts[b] .. starts[b+1] - 1 of the call's token operands. */
+typedef struct {
+    void *K, *V;             /* device: pages x kv_heads x page x d bfloat16 each */
+    const void *table;       /* device: seqs x max_pages int32 */
+    const void *lengths;     /* device: seqs int32 */
+    const void *starts;      /* device: seqs + 1 int32, ascending */
+    int64_t seqs, pages, max_pages, kv_heads, page, d;   /* page: a power of two up to 65536; d: 64 or 128 */
+    int64_t table_stride;    /* entries */
+    int64_t page_stride, head_stride, row_stride;        /* elements, of K and V alike; multiples of 8 */
+} cyc_cache;
+
+/* Writes the new tokens' keys and values, K and V: device, tokens x kv_heads x d bfloat16, into the cache: token t of sequence b
+ * becomes key lengths[b] - starts[b+1] + t.  strides (host): of token and head of K and of V in elements, four numbers, or NULL:
+ * dense.  lengths, starts and table are read on the device.  A token that belongs to no sequence, stands before key 0 or behind
+ * max_pages, or whose page is not in [0, pages), is not written; starts outside [0, tokens] leave their sequence unwritten.  Two tokens
+ * of one call that the table sends to the same place leave either.
+ * tokens or seqs == 0: CYC_OK, nothing done.  Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE, CYC_ERR_ALIAS (the cache
+ * overlaps K, V, table, lengths or starts, or keeps keys and values in the same place), CYC_ERR_LAUNCH. */
+int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64_t tokens, const int64_t *strides, void *stream);
+
+/* Attention of new tokens, one or many to a sequence, over the cache that holds them already: the mask and arithmetic of
+ * cyc_recurrence_attention_window with the queries of sequence b at the last starts[b+1] - starts[b] of its lengths[b] positions.
+ * Q: device, read only, O: device, written, tokens x heads x d bfloat16; strides (host): of token and head of Q and of O in
+ * elements, four numbers, or NULL: dense.  Pages that no query of the call sees (those a window has passed) are not read and their
+ * entries may hold anything.  Rows of O that belong to no sequence keep what they held.
+ * max_new (host): the most new tokens that any sequence brings, or 0: not known; it decides which kernels the call needs.
+ * Wrong numbers on the device give NaN, not faults: a sequence of more than max_new tokens, with a length below 0 or above max_pages * page,
+ * or with starts outside [0, tokens] has NaN in its rows; a table entry outside [0, pages) where a page is read puts NaN into the rows
+ * that see it and may put it into other rows of that sequence.  Where starts does not ascend, rows are undefined.
+ * workspace: as for cyc_recurrence_attention_window; cyc_attention_paged_workspace says how many bytes the call wants.
+ * Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE, CYC_ERR_ALIAS (O or workspace overlaps another operand), CYC_ERR_LAUNCH. */
+int64_t cyc_attention_paged_workspace(const cyc_cache *cache, int64_t tokens, int64_t heads, int64_t max_new, int64_t window,
+                                      int64_t sinks);
+int cyc_recurrence_attention_paged(const void *Q, const cyc_cache *cache, void *O, int64_t tokens, int64_t heads, const int64_t *strides,
+                                   int64_t max_new, int64_t window, int64_t sinks, void *workspace, int64_t workspace_bytes,
+                                   void *stream);
+
 /* Human-readable name of a cyc_status (static storage, never NULL). */
 const char *cyc_status_string(int status);
 

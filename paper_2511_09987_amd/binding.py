@@ -5,6 +5,7 @@ fallback: if the shared library is missing, the first call raises ImportError.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -15,6 +16,13 @@ CYC_ERR_WORKSPACE = 6
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libcyclotron_mm.so")
+
+
+class cyc_cache(ctypes.Structure):
+    """A cache of keys and values in pages and the sequences of a call (include/cyclotron_mm.h)."""
+    _fields_ = [(name, ctypes.c_void_p) for name in ("K", "V", "table", "lengths", "starts")] + \
+        [(name, ctypes.c_int64) for name in ("seqs", "pages", "max_pages", "kv_heads", "page", "d", "table_stride",
+                                             "page_stride", "head_stride", "row_stride")]
 
 
 def lib_path() -> str:
@@ -55,6 +63,21 @@ def _load() -> ctypes.CDLL:
     lib.cyc_recurrence_attention_split.restype = cint
     lib.cyc_attention_workspace.argtypes = [i64, i64, i64, i64]
     lib.cyc_attention_workspace.restype = i64
+    strides, cache = ctypes.POINTER(i64), ctypes.POINTER(cyc_cache)
+    lib.cyc_attention_window_workspace.argtypes = [i64] * 8
+    lib.cyc_attention_window_workspace.restype = i64
+    lib.cyc_recurrence_attention_window.argtypes = [ptr] * 5 + [i64] * 6 + [strides, i64, i64, ptr, i64, ptr]
+    lib.cyc_recurrence_attention_window.restype = cint
+    lib.cyc_attention_window_grad_workspace.argtypes = [i64] * 8
+    lib.cyc_attention_window_grad_workspace.restype = i64
+    lib.cyc_recurrence_attention_window_grad.argtypes = [ptr] * 9 + [i64] * 6 + [strides, i64, i64, ptr, i64, ptr]
+    lib.cyc_recurrence_attention_window_grad.restype = cint
+    lib.cyc_cache_append.argtypes = [ptr, ptr, cache, i64, strides, ptr]
+    lib.cyc_cache_append.restype = cint
+    lib.cyc_attention_paged_workspace.argtypes = [cache, i64, i64, i64, i64, i64]
+    lib.cyc_attention_paged_workspace.restype = i64
+    lib.cyc_recurrence_attention_paged.argtypes = [ptr, cache, ptr, i64, i64, strides, i64, i64, i64, ptr, i64, ptr]
+    lib.cyc_recurrence_attention_paged.restype = cint
     lib.cyc_status_string.argtypes = [cint]
     lib.cyc_status_string.restype = ctypes.c_char_p
     lib.cyc_version.argtypes = []
@@ -406,6 +429,261 @@ def recurrence_attention(Q, K, V, out=None, stream=None):
     else:
         st = cyc_recurrence_attention_split(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), batch, N, M, d, work.data_ptr(),
                                             wanted, s)
+    if st != CYC_OK:
+        raise CycError(st)
+    return out
+
+
+def _numbers(strides):
+    """Strides as the C ABI takes them (a sequence of ints, or None)."""
+    return None if strides is None else (ctypes.c_int64 * len(strides))(*strides)
+
+
+def cyc_attention_window_workspace(batch: int, heads: int, kv_heads: int, N: int, M: int, d: int, window: int, sinks: int) -> int:
+    """Bytes of workspace that cyc_recurrence_attention_window wants for these extents."""
+    return int(_lib().cyc_attention_window_workspace(batch, heads, kv_heads, N, M, d, window, sinks))
+
+
+def cyc_recurrence_attention_window(Q: int, K: int, V: int, O: int, lse: int, batch: int, heads: int, kv_heads: int, N: int, M: int, d: int,
+                                    strides, window: int, sinks: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> int:
+    """Raw call: device addresses as ints, strides twelve ints or None; returns the cyc_status."""
+    return int(_lib().cyc_recurrence_attention_window(Q, K, V, O, lse, batch, heads, kv_heads, N, M, d, _numbers(strides), window, sinks,
+                                                      workspace, workspace_bytes, stream))
+
+
+def cyc_attention_window_grad_workspace(batch: int, heads: int, kv_heads: int, N: int, M: int, d: int, window: int, sinks: int) -> int:
+    """Bytes of workspace that cyc_recurrence_attention_window_grad needs for these extents."""
+    return int(_lib().cyc_attention_window_grad_workspace(batch, heads, kv_heads, N, M, d, window, sinks))
+
+
+def cyc_recurrence_attention_window_grad(Q: int, K: int, V: int, O: int, lse: int, dO: int, dQ: int, dK: int, dV: int, batch: int, heads: int,
+                                         kv_heads: int, N: int, M: int, d: int, strides, window: int, sinks: int, workspace: int,
+                                         workspace_bytes: int, stream: int = 0) -> int:
+    """Raw call: device addresses as ints, strides twenty-four ints or None; returns the cyc_status."""
+    return int(_lib().cyc_recurrence_attention_window_grad(Q, K, V, O, lse, dO, dQ, dK, dV, batch, heads, kv_heads, N, M, d, _numbers(strides),
+                                                           window, sinks, workspace, workspace_bytes, stream))
+
+
+def cyc_cache_append(K: int, V: int, cache: cyc_cache, tokens: int, strides, stream: int = 0) -> int:
+    """Raw call: device addresses as ints, strides four ints or None; returns the cyc_status."""
+    return int(_lib().cyc_cache_append(K, V, cache, tokens, _numbers(strides), stream))
+
+
+def cyc_attention_paged_workspace(cache: cyc_cache, tokens: int, heads: int, max_new: int, window: int, sinks: int) -> int:
+    """Bytes of workspace that cyc_recurrence_attention_paged wants for these extents."""
+    return int(_lib().cyc_attention_paged_workspace(cache, tokens, heads, max_new, window, sinks))
+
+
+def cyc_recurrence_attention_paged(Q: int, cache: cyc_cache, O: int, tokens: int, heads: int, strides, max_new: int, window: int, sinks: int,
+                                   workspace: int = 0, workspace_bytes: int = 0, stream: int = 0) -> int:
+    """Raw call: device addresses as ints, strides four ints or None; returns the cyc_status."""
+    return int(_lib().cyc_recurrence_attention_paged(Q, cache, O, tokens, heads, _numbers(strides), max_new, window, sinks, workspace,
+                                                     workspace_bytes, stream))
+
+
+@contextlib.contextmanager
+def _on(tensor, stream):
+    """The tensor's device as the current one, and `stream`, where one is given, as its current stream: what is allocated inside
+    comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it."""
+    import torch
+    with torch.cuda.device(tensor.device):
+        if isinstance(stream, torch.cuda.Stream) and stream.device == tensor.device:
+            with torch.cuda.stream(stream):
+                yield
+        else:
+            yield
+
+
+def _place(tensor, stream):
+    """_on where it changes anything: entering it costs 3 us."""
+    import torch
+    return contextlib.nullcontext() if stream is None and tensor.device.index == torch.cuda.current_device() else _on(tensor, stream)
+
+
+def _mask_arguments(window, sinks):
+    """window and sinks as the C ABI takes them."""
+    if window is not None and window < 1:
+        raise ValueError(f"window must be at least 1, or None for no window; got {window}")
+    if sinks < 0:
+        raise ValueError(f"sinks must not be negative; got {sinks}")
+    return window or 0, sinks
+
+
+def _check_rows(named, shape):
+    """bfloat16 device tensors of `shape` whose rows a kernel can read 16 bytes at a time."""
+    import torch
+    for name, t in named:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor; there is no CPU path")
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
+        if t.stride(-1) != 1 and t.numel() or t.data_ptr() & 15 or any(s % 8 for s in t.stride()[:-1]):
+            raise ValueError(f"{name} needs contiguous rows at multiples of 16 bytes")
+
+
+def _same_device(tensors):
+    device = tensors[0].device
+    if any(t.device != device for t in tensors):
+        raise ValueError("all tensors must be on one device")
+
+
+def _attention_shapes(Q, K):
+    if Q.dim() != 4 or K.dim() != 4 or Q.shape[0] != K.shape[0] or Q.shape[3] != K.shape[3]:
+        raise ValueError(f"shape mismatch: Q {tuple(Q.shape)}, K {tuple(K.shape)}")
+    if Q.shape[3] not in (64, 128):
+        raise ValueError(f"the head dimension must be 64 or 128, got {Q.shape[3]}")
+    if K.shape[1] == 0 or Q.shape[1] % K.shape[1]:
+        raise ValueError(f"{Q.shape[1]} query heads do not divide among {K.shape[1]} key heads")
+
+
+def _all_strides(tensors):
+    return None if all(t.is_contiguous() for t in tensors) else [s for t in tensors for s in t.stride()[:-1]]
+
+
+def recurrence_attention_window(Q, K, V, window=None, sinks: int = 0, out=None, lse=None, stream=None):
+    """Tensor-level convenience: (O, lse) of causal attention with a sliding window and sinks.
+
+    Q: (batch, heads, N, d), K, V: (batch, kv_heads, M, d), torch.bfloat16 CUDA tensors with contiguous rows of d (64 or 128) and any
+    strides otherwise that are multiples of 8 (so views of (batch, N, heads, d) will do); heads a multiple of kv_heads.  The
+    queries are the last N of the M positions; position p sees the keys j <= p with p - j < window (None: all) or j < sinks.
+    Allocates O (bfloat16, like Q), lse (float32, (batch, heads, N): the logarithms of the sums, for the gradient) unless given, and
+    memory to split the keys of few queries over the chip, and forwards pointers to the C ABI on the current (or given) stream.
+    (Where that memory is not to be had the keys are not split, and the fp32 sums are added in another order.)
+    """
+    import torch
+    _attention_shapes(Q, K)
+    _check_rows((("Q", Q),), Q.shape)
+    _check_rows((("K", K), ("V", V)), K.shape)
+    window, sinks = _mask_arguments(window, sinks)
+    batch, heads, N, d = Q.shape
+    kv_heads, M = K.shape[1:3]
+    with _place(Q, stream):
+        if out is None:
+            out = torch.empty((batch, heads, N, d), dtype=torch.bfloat16, device=Q.device)
+        else:
+            _check_rows((("out", out),), Q.shape)
+        if lse is None:
+            lse = torch.empty((batch, heads, N), dtype=torch.float32, device=Q.device)
+        elif lse.shape != Q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
+            raise ValueError("lse has the wrong shape, dtype or layout")
+        _same_device((Q, K, V, out, lse))
+        s = _stream_handle(Q, stream)
+        wanted = cyc_attention_window_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
+        work = _memory(wanted, Q, stream) if wanted else None
+        st = cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), batch, heads, kv_heads,
+                                             N, M, d, _all_strides((Q, K, V, out)), window, sinks, 0 if work is None else work.data_ptr(),
+                                             0 if work is None else wanted, s)
+    if st != CYC_OK:
+        raise CycError(st)
+    return out, lse
+
+
+def recurrence_attention_window_grad(Q, K, V, O, lse, dO, window=None, sinks: int = 0, dQ=None, dK=None, dV=None, stream=None):
+    """Tensor-level convenience: (dQ, dK, dV) of recurrence_attention_window from what it returned and the gradient of O.
+
+    Q, K, V, window, sinks as in the forward call, O and lse what it returned, dO like O.  Allocates the gradients (bfloat16, like Q, K
+    and V) unless given and the memory that the call needs, and forwards pointers to the C ABI on the current (or given) stream.
+    """
+    import torch
+    _attention_shapes(Q, K)
+    _check_rows((("Q", Q), ("O", O), ("dO", dO)), Q.shape)
+    _check_rows((("K", K), ("V", V)), K.shape)
+    window, sinks = _mask_arguments(window, sinks)
+    batch, heads, N, d = Q.shape
+    kv_heads, M = K.shape[1:3]
+    if lse.shape != Q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
+        raise ValueError("lse has the wrong shape, dtype or layout")
+    with _place(Q, stream):
+        dQ = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device) if dQ is None else dQ
+        dK = torch.empty(K.shape, dtype=torch.bfloat16, device=Q.device) if dK is None else dK
+        dV = torch.empty(K.shape, dtype=torch.bfloat16, device=Q.device) if dV is None else dV
+        _check_rows((("dQ", dQ),), Q.shape)
+        _check_rows((("dK", dK), ("dV", dV)), K.shape)
+        operands = (Q, K, V, O, dO, dQ, dK, dV)
+        _same_device((*operands, lse))
+        s = _stream_handle(Q, stream)
+        wanted = cyc_attention_window_grad_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
+        work = _memory(wanted, Q, stream) if wanted else None
+        st = cyc_recurrence_attention_window_grad(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
+                                                  dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), batch, heads, kv_heads, N, M, d,
+                                                  _all_strides(operands), window, sinks, 0 if work is None else work.data_ptr(),
+                                                  0 if work is None else wanted, s)
+    if st != CYC_OK:
+        raise CycError(st)
+    return dQ, dK, dV
+
+
+def _cache(K_cache, V_cache, table, lengths, starts):
+    """The tensors of a cache, checked, as the C ABI takes them."""
+    import torch
+    if K_cache.dim() != 4 or K_cache.stride() != V_cache.stride():
+        raise ValueError("K_cache and V_cache must be (pages, kv_heads, page, d) with the same strides")
+    _check_rows((("K_cache", K_cache), ("V_cache", V_cache)), K_cache.shape)
+    for name, t, dims in (("table", table, 2), ("lengths", lengths, 1), ("starts", starts, 1)):
+        if not t.is_cuda or t.dtype != torch.int32 or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+            raise ValueError(f"{name} must be a device tensor of int32 with {dims} dimension(s) and contiguous rows")
+    pages, kv_heads, page, d = K_cache.shape
+    seqs, max_pages = table.shape
+    if lengths.shape[0] != seqs or starts.shape[0] != seqs + 1:
+        raise ValueError(f"{seqs} sequences need {seqs} lengths and {seqs + 1} starts, got {lengths.shape[0]} and {starts.shape[0]}")
+    if page < 1 or page & (page - 1) or page > 65536 or d not in (64, 128):
+        raise ValueError(f"pages hold a power of two of keys (up to 65536) of 64 or 128 elements, got {page} of {d}")
+    return cyc_cache(K_cache.data_ptr(), V_cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), starts.data_ptr(), seqs, pages, max_pages,
+                     kv_heads, page, d, table.stride(0), *K_cache.stride()[:3])
+
+
+def cache_append(K, V, K_cache, V_cache, table, lengths, starts, stream=None):
+    """Tensor-level convenience: writes the keys and values of new tokens into the pages of a cache.
+
+    K, V: (tokens, kv_heads, d), K_cache, V_cache: (pages, kv_heads, page, d), torch.bfloat16 CUDA tensors with contiguous rows and any
+    strides otherwise that are multiples of 8; table: (sequences, max_pages), lengths: (sequences,), starts: (sequences + 1,), torch.int32.
+    Rows starts[b] .. starts[b+1] - 1 of K and V become the last of the lengths[b] keys of sequence b; key j lies in row j % page of
+    page table[b, j // page].  Tokens without a place (no sequence, key, or page) are not written.  Allocates nothing.
+    """
+    import torch  # noqa: F401
+    cache = _cache(K_cache, V_cache, table, lengths, starts)
+    shape = (K.shape[0] if K.dim() else 0, K_cache.shape[1], K_cache.shape[3])
+    _check_rows((("K", K), ("V", V)), shape)
+    _same_device((K, V, K_cache, V_cache, table, lengths, starts))
+    with _place(K, stream):
+        st = cyc_cache_append(K.data_ptr(), V.data_ptr(), cache, shape[0], _all_strides((K, V)), _stream_handle(K, stream))
+    if st != CYC_OK:
+        raise CycError(st)
+
+
+def recurrence_attention_paged(Q, K_cache, V_cache, table, lengths, starts, window=None, sinks: int = 0, max_new=None, out=None, stream=None):
+    """Tensor-level convenience: attention of new tokens over a paged cache that holds their keys and values already (cache_append).
+
+    Q: (tokens, heads, d), torch.bfloat16; the cache, table, lengths and starts as in cache_append, heads a multiple of kv_heads; window
+    and sinks as in recurrence_attention_window.  Rows starts[b] .. starts[b+1] - 1 of Q are the last positions of sequence b.  max_new: the
+    most new tokens that any sequence brings, where the caller knows it: with 1, the usual step of a decoder, only the kernel for
+    few rows is launched (a sequence that brings more has NaN in its rows then).  Allocates O (bfloat16, like Q) unless given and memory to
+    split the keys over the chip, and forwards pointers to the C ABI on the current (or given) stream.
+    """
+    import torch
+    cache = _cache(K_cache, V_cache, table, lengths, starts)
+    if Q.dim() != 3 or Q.shape[2] != K_cache.shape[3]:
+        raise ValueError(f"shape mismatch: Q {tuple(Q.shape)}, K_cache {tuple(K_cache.shape)}")
+    _check_rows((("Q", Q),), Q.shape)
+    window, sinks = _mask_arguments(window, sinks)
+    if max_new is not None and max_new < 1:
+        raise ValueError(f"max_new must be at least 1, or None; got {max_new}")
+    tokens, heads, d = Q.shape
+    if cache.kv_heads == 0 or heads % cache.kv_heads:
+        raise ValueError(f"{heads} query heads do not divide among {cache.kv_heads} key heads")
+    with _place(Q, stream):
+        if out is None:
+            out = torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=Q.device)
+        else:
+            _check_rows((("out", out),), Q.shape)
+        _same_device((Q, K_cache, V_cache, table, lengths, starts, out))
+        s = _stream_handle(Q, stream)
+        wanted = cyc_attention_paged_workspace(cache, tokens, heads, max_new or 0, window, sinks)
+        work = _memory(wanted, Q, stream) if wanted else None
+        st = cyc_recurrence_attention_paged(Q.data_ptr(), cache, out.data_ptr(), tokens, heads, _all_strides((Q, out)), max_new or 0, window,
+                                            sinks, 0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)
     if st != CYC_OK:
         raise CycError(st)
     return out

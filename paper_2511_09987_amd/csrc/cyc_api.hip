@@ -2,10 +2,13 @@
 // the choice of kernel.  No device work happens here except the launches.
 #include "../../include/cyclotron_mm.h"
 #include "cyc_internal.h"
+#include "cyc_window.h"
 
 #include <cstdlib>
 #include <cstring>
 #include <atomic>
+#include <algorithm>
+#include <climits>
 
 namespace {
 
@@ -270,6 +273,149 @@ int cholesky(const void *A, void *L, void *Lh, int64_t n, int64_t nb, void *stre
     return e == hipSuccess ? CYC_OK : CYC_ERR_LAUNCH;
 }
 
+// ---- attention with a window: operands of batch x heads x rows x d bfloat16 by strides
+struct Operand {
+    const void *p;
+    int64_t extent[3], stride[3];        // batch, head, row; elements
+    bool written;
+    int64_t elements() const { return extent[0] * extent[1] * extent[2]; }
+};
+
+// bytes from an operand's first element to its last
+int64_t span_of(const Operand &x, int64_t d)
+{
+    if (x.elements() == 0) return 0;
+    int64_t last = d;
+    for (int i = 0; i < 3; ++i) last += (x.extent[i] - 1) * x.stride[i];
+    return last * 2;
+}
+
+// strides that rows of 16-byte chunks can have, spans that 64-bit offsets hold; what is written does not meet itself
+bool strides_ok(const Operand &x, int64_t d)
+{
+    int64_t total = d, t;
+    for (int i = 0; i < 3; ++i) {
+        if (x.stride[i] < 0 || x.stride[i] % 8 || !mul_ok(x.extent[i], x.stride[i], &t)) return false;
+        if ((total += t) > kMaxElems) return false;
+    }
+    if (!x.written || x.elements() == 0) return true;
+    int order[3] = {0, 1, 2};
+    std::sort(order, order + 3, [&](int a, int b) { return x.stride[a] < x.stride[b]; });
+    int64_t reach = d;
+    for (int i : order) {
+        if (x.extent[i] == 1) continue;
+        if (x.stride[i] < reach) return false;
+        reach += (x.extent[i] - 1) * x.stride[i];
+    }
+    return true;
+}
+
+cyc::Strided strided(const Operand &x) { return {(const char *)x.p, x.stride[0] * 2, x.stride[1] * 2, x.stride[2] * 2}; }
+
+int clamped(int64_t x) { return (int)std::min<int64_t>(x, INT_MAX); }
+
+// extents and mask of cyc_recurrence_attention_window and its gradient; false where they are refused
+bool window_extents(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d, int64_t window, int64_t sinks, cyc::WindowProblem *p)
+{
+    if (batch < 0 || heads < 0 || kv_heads < 0 || N < 0 || M < 0 || window < 0 || sinks < 0 || (d != 64 && d != 128)) return false;
+    if (heads > 0 && (kv_heads == 0 || heads % kv_heads)) return false;
+    const int64_t group = heads > 0 ? heads / kv_heads : 1;
+    int64_t t;
+    if (M >= (1 << 30) || !mul_ok(group, N, &t) || t >= (1 << 30) || !mul_ok(batch, std::max(heads, kv_heads), &t) || t >= (1 << 24)) return false;
+    *p = cyc::WindowProblem{};
+    p->batch = (int)batch, p->heads = (int)heads, p->kv_heads = (int)kv_heads, p->group = (int)group;
+    p->N = (int)N, p->M = (int)M, p->d = (int)d;
+    p->window = window == 0 ? INT_MAX : clamped(window), p->sinks = clamped(sinks);
+    return true;
+}
+
+// The operands of a call by pointer: `count` of them, Q-like (batch x heads x N) or K-like (batch x kv_heads x M).
+struct Named {
+    const void *p;
+    bool keys, written;
+};
+int window_operands(const Named *named, int count, const cyc::WindowProblem &p, const int64_t *strides, const void *lse, bool lse_written, const void *workspace,
+                    int64_t workspace_bytes, Operand *x)
+{
+    for (int i = 0; i < count; ++i) {
+        const int64_t heads = named[i].keys ? p.kv_heads : p.heads, rows = named[i].keys ? p.M : p.N;
+        x[i] = {named[i].p, {p.batch, heads, rows}, {heads * rows * p.d, rows * p.d, p.d}, named[i].written};
+        if (strides) std::copy(strides + 3 * i, strides + 3 * i + 3, x[i].stride);
+        if (!strides_ok(x[i], p.d)) return CYC_ERR_SHAPE;
+    }
+    for (int i = 0; i < count; ++i)
+        if (!x[i].p && x[i].elements()) return CYC_ERR_NULL;
+    for (int i = 0; i < count; ++i)
+        if ((uintptr_t)x[i].p & 15) return CYC_ERR_SHAPE;
+    if (((uintptr_t)lse & 3) || !workspace_ok(workspace, workspace_bytes)) return CYC_ERR_SHAPE;
+    const int64_t lse_bytes = (int64_t)p.batch * p.heads * p.N * 4;
+    if (overlaps(lse, lse_bytes, workspace, workspace_bytes)) return CYC_ERR_ALIAS;
+    for (int i = 0; i < count; ++i) {
+        const int64_t bytes = span_of(x[i], p.d);
+        if (overlaps(x[i].p, bytes, workspace, workspace_bytes)) return CYC_ERR_ALIAS;
+        if ((x[i].written || lse_written) && overlaps(x[i].p, bytes, lse, lse_bytes)) return CYC_ERR_ALIAS;
+        for (int j = 0; j < count; ++j)
+            if (j != i && x[i].written && overlaps(x[i].p, bytes, x[j].p, span_of(x[j], p.d))) return CYC_ERR_ALIAS;
+    }
+    return CYC_OK;
+}
+
+// ---- the paged cache
+bool log2_of(int64_t x, int *shift)
+{
+    for (*shift = 0; *shift <= 16; ++*shift)
+        if (x == (int64_t)1 << *shift) return true;
+    return false;
+}
+
+// extents of a cache; pointers are looked at separately
+bool cache_extents(const cyc_cache &c, int64_t tokens, int *shift)
+{
+    if (c.seqs < 0 || c.pages < 1 || c.max_pages < 1 || c.kv_heads < 1 || c.table_stride < 0 || tokens < 0 || (c.d != 64 && c.d != 128)) return false;
+    if (!log2_of(c.page, shift) || c.seqs >= (1 << 24) || c.pages > INT_MAX || c.kv_heads >= (1 << 16) || c.max_pages > (1 << 30)) return false;
+    int64_t t;
+    if (!mul_ok(c.max_pages, c.page, &t) || t >= (1 << 30) || tokens >= (1 << 30) || !mul_ok(c.seqs, c.table_stride, &t)) return false;
+    return strides_ok({nullptr, {c.pages, c.kv_heads, c.page}, {c.page_stride, c.head_stride, c.row_stride}, true}, c.d);
+}
+int64_t cache_span(const cyc_cache &c) { return span_of({nullptr, {c.pages, c.kv_heads, c.page}, {c.page_stride, c.head_stride, c.row_stride}, true}, c.d); }
+
+bool overlaps_indices(const cyc_cache &c, const void *p, int64_t bytes)
+{
+    return overlaps(p, bytes, c.table, ((c.seqs - 1) * c.table_stride + c.max_pages) * 4) || overlaps(p, bytes, c.lengths, c.seqs * 4) ||
+           overlaps(p, bytes, c.starts, (c.seqs + 1) * 4);
+}
+
+// strides of two operands of tokens x heads x d
+bool token_strides(const int64_t *strides, const void *a, const void *b, int64_t tokens, int64_t heads, int64_t d, bool b_written, Operand *x)
+{
+    for (int i = 0; i < 2; ++i) {
+        x[i] = {i ? b : a, {1, tokens, heads}, {0, heads * d, d}, i && b_written};
+        if (strides) x[i].stride[1] = strides[2 * i], x[i].stride[2] = strides[2 * i + 1];
+        if (!strides_ok(x[i], d)) return false;
+    }
+    return true;
+}
+
+bool paged_extents(const cyc_cache &c, int64_t tokens, int64_t heads, int64_t max_new, int64_t window, int64_t sinks, cyc::PagedProblem *p)
+{
+    int shift;
+    if (!cache_extents(c, tokens, &shift) || heads < 0 || heads % c.kv_heads || max_new < 0 || window < 0 || sinks < 0) return false;
+    int64_t t;
+    if (heads >= (1 << 20) || !mul_ok(tokens, heads, &t) || t >= ((int64_t)1 << 32)) return false;
+    const int64_t group = std::max<int64_t>(heads / c.kv_heads, 1);
+    if (tokens * group >= (1 << 30)) return false;
+    *p = cyc::PagedProblem{};
+    p->tokens = (int)tokens, p->seqs = (int)c.seqs, p->heads = (int)heads, p->kv_heads = (int)c.kv_heads, p->group = (int)group, p->d = (int)c.d;
+    p->pages = (int)c.pages, p->page_shift = shift, p->max_pages = (int)c.max_pages;
+    p->max_new = (int)(max_new == 0 ? tokens : std::min(max_new, tokens));
+    p->window = window == 0 ? INT_MAX : clamped(window), p->sinks = clamped(sinks);
+    p->page_bytes = c.page_stride * 2, p->head_bytes = c.head_stride * 2, p->row_bytes = c.row_stride * 2;
+    p->table_stride = c.table_stride;
+    p->K = (const char *)c.K, p->V = (const char *)c.V;
+    p->table = (const int *)c.table, p->lengths = (const int *)c.lengths, p->starts = (const int *)c.starts;
+    return true;
+}
+
 }  // namespace
 
 namespace cyc {
@@ -417,6 +563,123 @@ int cyc_recurrence_attention_split(const void *Q, const void *K, const void *V, 
                                                                                                                         : CYC_ERR_LAUNCH;
 }
 
+int64_t cyc_attention_window_workspace(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d, int64_t window,
+                                       int64_t sinks)
+{
+    cyc::WindowProblem p;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || batch == 0 || heads == 0 || N == 0) return 0;
+    return cyc::window_workspace_bytes(p);
+}
+
+int cyc_recurrence_attention_window(const void *Q, const void *K, const void *V, void *O, void *lse, int64_t batch, int64_t heads,
+                                    int64_t kv_heads, int64_t N, int64_t M, int64_t d, const int64_t *strides, int64_t window,
+                                    int64_t sinks, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    cyc::WindowProblem p;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p)) return CYC_ERR_SHAPE;
+    if (batch == 0 || heads == 0 || N == 0) return CYC_OK;
+    if (!workspace || workspace_bytes < 0) workspace_bytes = 0;
+    Operand x[4];
+    const Named named[4] = {{Q, false, false}, {K, true, false}, {V, true, false}, {O, false, true}};
+    if (int st = window_operands(named, 4, p, strides, lse, true, workspace, workspace_bytes, x); st != CYC_OK) return st;
+    p.Q = strided(x[0]), p.K = strided(x[1]), p.V = strided(x[2]), p.O = strided(x[3]);
+    p.lse = (float *)lse;
+    return cyc::launch_window(p, workspace, workspace_bytes, (hipStream_t)stream) == hipSuccess ? CYC_OK : CYC_ERR_LAUNCH;
+}
+
+int64_t cyc_attention_window_grad_workspace(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
+                                            int64_t window, int64_t sinks)
+{
+    cyc::WindowProblem p;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || batch == 0 || heads == 0 || kv_heads * M >= (1 << 30)) return 0;
+    return cyc::window_grad_workspace_bytes(p);
+}
+
+int cyc_recurrence_attention_window_grad(const void *Q, const void *K, const void *V, const void *O, const void *lse, const void *dO,
+                                         void *dQ, void *dK, void *dV, int64_t batch, int64_t heads, int64_t kv_heads, int64_t N,
+                                         int64_t M, int64_t d, const int64_t *strides, int64_t window, int64_t sinks, void *workspace,
+                                         int64_t workspace_bytes, void *stream)
+{
+    cyc::WindowProblem p;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || kv_heads * M >= (1 << 30)) return CYC_ERR_SHAPE;
+    if (batch == 0 || heads == 0 || (N == 0 && M == 0)) return CYC_OK;
+    if (!workspace || workspace_bytes < 0) workspace_bytes = 0;
+    Operand x[8];
+    const Named named[8] = {{Q, false, false}, {K, true, false}, {V, true, false}, {O, false, false},
+                            {dO, false, false}, {dQ, false, true}, {dK, true, true}, {dV, true, true}};
+    if (int st = window_operands(named, 8, p, strides, lse, false, workspace, workspace_bytes, x); st != CYC_OK) return st;
+    if (!lse && N > 0) return CYC_ERR_NULL;
+    if (workspace_bytes < cyc::window_grad_workspace_bytes(p)) return CYC_ERR_WORKSPACE;
+    p.Q = strided(x[0]), p.K = strided(x[1]), p.V = strided(x[2]), p.O = strided(x[3]);
+    p.dO = strided(x[4]), p.dQ = strided(x[5]), p.dK = strided(x[6]), p.dV = strided(x[7]);
+    p.lse = (float *)const_cast<void *>(lse);
+    return cyc::launch_window_grad(p, workspace, workspace_bytes, (hipStream_t)stream) == hipSuccess ? CYC_OK : CYC_ERR_LAUNCH;
+}
+
+int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64_t tokens, const int64_t *strides, void *stream)
+{
+    if (!cache) return CYC_ERR_NULL;
+    const cyc_cache &c = *cache;
+    int shift;
+    Operand x[2];
+    int64_t t;
+    if (!cache_extents(c, tokens, &shift) || !mul_ok(tokens, c.kv_heads * c.d, &t) || !token_strides(strides, K, V, tokens, c.kv_heads, c.d, false, x))
+        return CYC_ERR_SHAPE;
+    if (t / 8 >= ((int64_t)1 << 38)) return CYC_ERR_SHAPE;        // (a grid of 2^31 workgroups of 128 chunks)
+    if (tokens == 0 || c.seqs == 0) return CYC_OK;
+    if (!K || !V || !c.K || !c.V || !c.table || !c.lengths || !c.starts) return CYC_ERR_NULL;
+    if (((uintptr_t)K | (uintptr_t)V | (uintptr_t)c.K | (uintptr_t)c.V) & 15 || ((uintptr_t)c.table | (uintptr_t)c.lengths | (uintptr_t)c.starts) & 3)
+        return CYC_ERR_SHAPE;
+    const int64_t span = cache_span(c);
+    if (c.K == c.V) return CYC_ERR_ALIAS;
+    for (const void *pool : {c.K, c.V}) {
+        for (const Operand &o : x)
+            if (overlaps(pool, span, o.p, span_of(o, c.d))) return CYC_ERR_ALIAS;
+        if (overlaps_indices(c, pool, span)) return CYC_ERR_ALIAS;
+    }
+    cyc::AppendProblem p{};
+    p.K = (const char *)K, p.V = (const char *)V, p.K_cache = (char *)c.K, p.V_cache = (char *)c.V;
+    p.k_token = x[0].stride[1] * 2, p.k_head = x[0].stride[2] * 2, p.v_token = x[1].stride[1] * 2, p.v_head = x[1].stride[2] * 2;
+    p.page_bytes = c.page_stride * 2, p.head_bytes = c.head_stride * 2, p.row_bytes = c.row_stride * 2, p.table_stride = c.table_stride;
+    p.table = (const int *)c.table, p.lengths = (const int *)c.lengths, p.starts = (const int *)c.starts;
+    p.tokens = (int)tokens, p.seqs = (int)c.seqs, p.kv_heads = (int)c.kv_heads, p.d = (int)c.d;
+    p.pages = (int)c.pages, p.page_shift = shift, p.max_pages = (int)c.max_pages;
+    return cyc::launch_append(p, (hipStream_t)stream) == hipSuccess ? CYC_OK : CYC_ERR_LAUNCH;
+}
+
+int64_t cyc_attention_paged_workspace(const cyc_cache *cache, int64_t tokens, int64_t heads, int64_t max_new, int64_t window,
+                                      int64_t sinks)
+{
+    cyc::PagedProblem p;
+    if (!cache || !paged_extents(*cache, tokens, heads, max_new, window, sinks, &p) || tokens == 0 || heads == 0 || cache->seqs == 0) return 0;
+    return cyc::paged_workspace_bytes(p);
+}
+
+int cyc_recurrence_attention_paged(const void *Q, const cyc_cache *cache, void *O, int64_t tokens, int64_t heads, const int64_t *strides,
+                                   int64_t max_new, int64_t window, int64_t sinks, void *workspace, int64_t workspace_bytes, void *stream)
+{
+    if (!cache) return CYC_ERR_NULL;
+    const cyc_cache &c = *cache;
+    cyc::PagedProblem p;
+    Operand x[2];
+    if (!paged_extents(c, tokens, heads, max_new, window, sinks, &p) || !token_strides(strides, Q, O, tokens, heads, c.d, true, x)) return CYC_ERR_SHAPE;
+    if (tokens == 0 || heads == 0 || c.seqs == 0) return CYC_OK;
+    if (!Q || !O || !c.K || !c.V || !c.table || !c.lengths || !c.starts) return CYC_ERR_NULL;
+    if (!workspace || workspace_bytes < 0) workspace_bytes = 0;
+    if (((uintptr_t)Q | (uintptr_t)O | (uintptr_t)c.K | (uintptr_t)c.V | (uintptr_t)workspace) & 15 ||
+        ((uintptr_t)c.table | (uintptr_t)c.lengths | (uintptr_t)c.starts) & 3)
+        return CYC_ERR_SHAPE;
+    const int64_t span = cache_span(c), qspan = span_of(x[0], c.d), ospan = span_of(x[1], c.d);
+    if (overlaps(O, ospan, Q, qspan) || overlaps(O, ospan, c.K, span) || overlaps(O, ospan, c.V, span) || overlaps_indices(c, O, ospan))
+        return CYC_ERR_ALIAS;
+    if (overlaps(workspace, workspace_bytes, Q, qspan) || overlaps(workspace, workspace_bytes, O, ospan) ||
+        overlaps(workspace, workspace_bytes, c.K, span) || overlaps(workspace, workspace_bytes, c.V, span) || overlaps_indices(c, workspace, workspace_bytes))
+        return CYC_ERR_ALIAS;
+    p.Q = (const char *)Q, p.O = (char *)O;
+    p.q_token = x[0].stride[1] * 2, p.q_head = x[0].stride[2] * 2, p.o_token = x[1].stride[1] * 2, p.o_head = x[1].stride[2] * 2;
+    return cyc::launch_paged(p, workspace, workspace_bytes, (hipStream_t)stream) == hipSuccess ? CYC_OK : CYC_ERR_LAUNCH;
+}
+
 const char *cyc_kernel_name(const void *A, const void *B, const void *C, int64_t batch, int64_t M, int64_t K,
                             int64_t N, int64_t strideA, int64_t strideB, int64_t strideC, int dtype)
 {
@@ -451,7 +714,7 @@ const char *cyc_status_string(int status)
     return "unknown cyc_status";
 }
 
-int cyc_version(void) { return 300; }
+int cyc_version(void) { return 400; }
 
 int cyc_diag_set_wait_limit(int64_t polls)
 {

@@ -1,0 +1,274 @@
+"""GPU parity of attention with a window and sinks, and of its gradient, against the definition in 64 bits.
+
+Every element is held to the bounds derived in attention_reference.py."""
+import math
+
+import pytest
+import torch
+
+import attention_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2511_09987_amd as pkg
+    return pkg
+
+
+def normal(shape, seed, sigma=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return torch.empty(shape, dtype=torch.bfloat16, device=DEV).normal_(0.0, sigma, generator=g)
+
+
+def operands(batch, heads, kv, N, M, d, seed):
+    return normal((batch, heads, N, d), seed), normal((batch, kv, M, d), seed + 1), normal((batch, kv, M, d), seed + 2)
+
+
+# batch, heads, kv_heads, N, M, d, window, sinks
+CASES = [
+    (1, 1, 1, 1, 1, 64, None, 0), (1, 2, 1, 1, 1, 128, 1, 0), (2, 4, 2, 1, 77, 128, None, 0), (1, 3, 1, 5, 3, 64, None, 0),
+    (1, 2, 2, 70, 70, 64, 1, 0), (1, 2, 1, 130, 130, 128, 64, 1), (1, 4, 4, 64, 64, 64, 32, 4), (2, 6, 2, 129, 257, 64, 100, 70),
+    (1, 8, 1, 33, 1000, 128, 256, 300), (1, 5, 5, 300, 300, 128, None, 0), (1, 2, 1, 7, 0, 64, None, 0), (3, 12, 4, 200, 333, 64, 65, 17),
+    (1, 16, 1, 1, 5000, 128, None, 0), (1, 2, 1, 513, 2100, 64, 2000, 4), (1, 2, 2, 100, 90, 128, 16, 3), (1, 7, 1, 45, 300, 128, 5000, 9),
+    (1, 1, 1, 257, 257, 128, 128, 1000), (2, 40, 1, 3, 129, 64, 128, 0), (1, 4, 2, 400, 64, 64, 7, 2), (1, 2, 1, 1, 4097, 64, 1024, 5),
+    (5, 3, 3, 17, 65, 128, 33, 31), (1, 1, 1, 128, 128, 64, 129, 0), (1, 9, 3, 31, 31, 128, 64, 64), (1, 64, 8, 2, 1500, 128, 600, 65),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_forward(lib, case):
+    batch, heads, kv, N, M, d, window, sinks = case
+    Q, K, V = operands(batch, heads, kv, N, M, d, 11 * N + M)
+    O, lse = lib.recurrence_attention_window(Q, K, V, window, sinks)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, window, sinks)
+    ref.within(O, want, bound, "O")
+    ref.within(lse, wlse, lbound, "lse")
+    again, lagain = lib.recurrence_attention_window(Q, K, V, window, sinks)
+    assert torch.equal(O.view(torch.int16), again.view(torch.int16)) and torch.equal(lse.view(torch.int32), lagain.view(torch.int32))
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_gradient(lib, case):
+    batch, heads, kv, N, M, d, window, sinks = case
+    Q, K, V = operands(batch, heads, kv, N, M, d, 13 * N + M)
+    dO = normal(Q.shape, 17 * N + M)
+    O, lse, _, _ = ref.forward(Q, K, V, window, sinks)
+    O, lse = O.to(torch.bfloat16), lse.float()
+    got = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window, sinks)
+    want, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bounds):
+        ref.within(g, w, b, name)
+    again = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window, sinks)
+    for g, a in zip(got, again):
+        assert torch.equal(g.view(torch.int16), a.view(torch.int16))
+
+
+def test_gradient_against_differences_of_the_forward(lib):
+    """The whole step as a program makes it, O and lse from the call: <dQ, u> against central differences in 64 bits.  O is
+    rounded, which moves D_i by up to 2^-8 sum_c |dO_c O_c| and dS_ij by P_ij times that."""
+    case = (1, 4, 2, 40, 90, 64, 33, 5)
+    batch, heads, kv, N, M, d, window, sinks = case
+    Q, K, V = operands(batch, heads, kv, N, M, d, 5)
+    dO = normal(Q.shape, 6)
+    O, lse = lib.recurrence_attention_window(Q, K, V, window, sinks)
+    got = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window, sinks)
+    _, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    O64, lse64, obound, _ = ref.forward(Q, K, V, window, sinks)
+    moved = (dO.double().abs() * obound).sum(-1, keepdim=True)                   # of D
+    zero = torch.zeros_like(dO)
+    # P times the shift of D, through K and Q: the reference gradient of |.| operands with dO = 0 and D = -moved
+    P = torch.exp((torch.where(ref.visible(N, M, window, sinks, DEV), 0.0, -math.inf) +
+                   Q.double() @ K.double().repeat_interleave(2, 1).transpose(-1, -2) / 8.0) - lse64[..., None])
+    extra = ((P * moved) @ K.double().repeat_interleave(2, 1).abs() / 8.0,
+             ((P * moved).transpose(-1, -2) @ Q.double().abs()).view(batch, kv, 2, M, d).sum(2) / 8.0, zero[:, :kv, :1].double() * 0)
+    h = 1e-4
+    for which, (g, b, e) in enumerate(zip(got, bounds, extra)):
+        u = torch.randn(g.shape, dtype=torch.float64, generator=torch.Generator().manual_seed(which)).to(DEV)
+        ends = []
+        for sign in (1, -1):
+            x = [Q.double(), K.double(), V.double()]
+            x[which] = x[which] + sign * h * u
+            ends.append((ref.forward(*x, window, sinks)[0] * dO.double()).sum().item())
+        diff = (ends[0] - ends[1]) / (2 * h)
+        allowed = ((b + e) * u.abs()).sum().item() + 1e-5 * (1 + abs(diff))
+        assert abs((g.double() * u).sum().item() - diff) <= allowed, which
+
+
+@pytest.mark.parametrize("d", (64, 128))
+@pytest.mark.parametrize("rising", (True, False))
+def test_scores_that_rise_or_fall_along_the_keys(lib, d, rising):
+    """Every key's score is 2 above (below) the last one's, exactly: the reference of the running sum has to move all the time."""
+    M = 250
+    c = torch.arange(M, device=DEV, dtype=torch.float32) * (0.25 if d == 64 else 0.125)
+    c = c if rising else c.flip(0)
+    K = c[:, None].expand(M, d).to(torch.bfloat16).view(1, 1, M, d)
+    Q = torch.ones((1, 2, M, d), dtype=torch.bfloat16, device=DEV)
+    V = normal((1, 1, M, d), 3)
+    for window, sinks in ((None, 0), (40, 3)):
+        O, lse = lib.recurrence_attention_window(Q, K, V, window, sinks)
+        want, wlse, bound, lbound = ref.forward(Q, K, V, window, sinks)
+        ref.within(O, want, bound, "O")
+        ref.within(lse, wlse, lbound, "lse")
+
+
+@pytest.mark.parametrize("bad", (float("nan"), float("inf"), -float("inf")))
+@pytest.mark.parametrize("d", (64, 128))
+def test_what_is_masked_never_reaches_a_query(lib, bad, d):
+    """Keys and values that are no numbers: the queries that see them get NaN or infinities, all others what they get without."""
+    N = M = 300
+    window, sinks = 50, 3
+    Q, K, V = operands(1, 2, 1, N, M, d, 21)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, window, sinks)
+    seen = ref.visible(N, M, window, sinks, DEV)
+    for at in (1, 17, 64, 130, 255, 299):
+        Kb, Vb = K.clone(), V.clone()
+        Vb[:, :, at] = bad
+        Kb[:, :, at, ::3] = bad
+        clean = ~seen[:, at]
+        O, lse = lib.recurrence_attention_window(Q, Kb, Vb, window, sinks)
+        ref.within(O[:, :, clean], want[:, :, clean], bound[:, :, clean], f"O beside key {at}")
+        ref.within(lse[:, :, clean], wlse[:, :, clean], lbound[:, :, clean], f"lse beside key {at}")
+        Vb[:, :, at] = bad
+        O, _ = lib.recurrence_attention_window(Q, K, Vb, window, sinks)          # finite scores: every query that sees it
+        ref.within(O[:, :, clean], want[:, :, clean], bound[:, :, clean], f"O beside value {at}")
+        assert not torch.isfinite(O[:, :, ~clean]).any()
+
+
+def test_nan_in_keys_that_no_query_sees(lib):
+    """A window has passed the first keys: they may hold anything, and take no gradient."""
+    N, M, window = 40, 400, 64
+    Q, K, V = operands(2, 4, 2, N, M, 128, 31)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, window, 0)
+    K[:, :, :M - N - window] = float("nan")
+    V[:, :, :M - N - window] = float("inf")
+    O, lse = lib.recurrence_attention_window(Q, K, V, window)
+    ref.within(O, want, bound, "O")
+    ref.within(lse, wlse, lbound, "lse")
+    dO = normal(Q.shape, 32)
+    dQ, dK, dV = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window)
+    assert torch.isfinite(dQ).all() and torch.isfinite(dK).all() and torch.isfinite(dV).all()
+    assert not dK[:, :, :M - N - window].any() and not dV[:, :, :M - N - window].any()
+
+
+def test_gradients_beside_what_is_masked(lib):
+    """One key, one query's dO, one query without numbers: every gradient that does not meet them in a visible pair stays what it is."""
+    N = M = 200
+    window, sinks = 40, 2
+    Q, K, V = operands(1, 2, 1, N, M, 128, 41)
+    dO = normal(Q.shape, 42)
+    O, lse, _, _ = ref.forward(Q, K, V, window, sinks)
+    O, lse = O.to(torch.bfloat16), lse.float()
+    want, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    seen = ref.visible(N, M, window, sinks, DEV)
+    for at in (70, 133, 199):
+        for which in ("K", "V", "Q", "dO"):
+            x = {"Q": Q, "K": K, "V": V, "dO": dO}
+            x[which] = x[which].clone()
+            x[which][:, :, at] = float("nan")
+            dQ, dK, dV = lib.recurrence_attention_window_grad(x["Q"], x["K"], x["V"], O, lse, x["dO"], window, sinks)
+            if which in ("K", "V"):        # queries that do not see the key; keys that share no query with it
+                queries = ~seen[:, at]
+                keys = ~(seen[seen[:, at]].any(0))
+            else:
+                queries = torch.ones(N, dtype=torch.bool, device=DEV)
+                queries[at] = False
+                keys = ~seen[at]
+            ref.within(dQ[:, :, queries], want[0][:, :, queries], bounds[0][:, :, queries], f"dQ, {which} {at}")
+            ref.within(dK[:, :, keys], want[1][:, :, keys], bounds[1][:, :, keys], f"dK, {which} {at}")
+            ref.within(dV[:, :, keys], want[2][:, :, keys], bounds[2][:, :, keys], f"dV, {which} {at}")
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_views(lib, d):
+    """(batch, rows, heads, d) tensors, one buffer for queries, keys and values, keys that the whole batch shares; results into views."""
+    batch, heads, kv, N, window, sinks = 2, 6, 2, 150, 60, 3
+    fused = normal((batch, N, heads + 2 * kv, d), 51)
+    Q, K, V = (t.transpose(1, 2) for t in fused.split((heads, kv, kv), 2))
+    out = torch.zeros((batch, N, heads, d), dtype=torch.bfloat16, device=DEV).transpose(1, 2)
+    O, lse = lib.recurrence_attention_window(Q, K, V, window, sinks, out=out)
+    assert O is out
+    want, wlse, bound, lbound = ref.forward(Q, K, V, window, sinks)
+    ref.within(O, want, bound, "O")
+    ref.within(lse, wlse, lbound, "lse")
+    dO = normal((batch, N, heads, d), 52).transpose(1, 2)
+    grads = [torch.zeros((batch, N, h, d), dtype=torch.bfloat16, device=DEV).transpose(1, 2) for h in (heads, kv, kv)]
+    lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window, sinks, *grads)
+    want, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    for name, g, w, b in zip(("dQ", "dK", "dV"), grads, want, bounds):
+        ref.within(g, w, b, name)
+    # keys of stride 0 along the batch, gradients of each batch element
+    Ks, Vs = K[:1].expand(batch, -1, -1, -1), V[:1].expand(batch, -1, -1, -1)
+    O, lse = lib.recurrence_attention_window(Q, Ks, Vs, window, sinks)
+    want, wlse, bound, lbound = ref.forward(Q, Ks, Vs, window, sinks)
+    ref.within(O, want, bound, "O, shared keys")
+    got = lib.recurrence_attention_window_grad(Q, Ks, Vs, O, lse, dO, window, sinks)
+    want, bounds = ref.gradient(Q, Ks, Vs, O, lse, dO, window, sinks)
+    for name, g, w, b in zip(("dQ", "dK", "dV"), got, want, bounds):
+        ref.within(g, w, b, name + ", shared keys")
+
+
+def test_refusals_of_device_tensors(lib):
+    Q, K, V = operands(1, 2, 1, 8, 8, 64, 61)
+    call = lib.recurrence_attention_window
+    with pytest.raises(ValueError, match="bfloat16"):
+        call(Q.float(), K, V)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        call(normal((1, 2, 8, 128), 1)[..., ::2], K, V)
+    with pytest.raises(ValueError, match="contiguous rows"):
+        call(normal((1, 2, 8, 68), 1)[..., :64], K, V)
+    with pytest.raises(ValueError, match="shape mismatch"):
+        call(Q, K, V[:, :, :7])
+    with pytest.raises(ValueError, match="window"):
+        call(Q, K, V, 0)
+    with pytest.raises(ValueError, match="sinks"):
+        call(Q, K, V, 4, -1)
+    with pytest.raises(ValueError, match="lse"):
+        call(Q, K, V, lse=torch.zeros((1, 2, 8), dtype=torch.float64, device=DEV))
+    with pytest.raises(lib.CycError, match="ALIAS"):
+        call(Q, K, V, out=Q)
+    with pytest.raises(lib.CycError, match="SHAPE"):
+        call(Q, K, V, out=normal((1, 1, 8, 64), 1).expand(1, 2, 8, 64))
+
+
+def test_another_stream_and_no_lse(lib):
+    Q, K, V = operands(2, 4, 2, 300, 300, 64, 81)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, 77, 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    O, lse = lib.recurrence_attention_window(Q, K, V, 77, 2, stream=side)
+    dO = normal(Q.shape, 82)
+    side.wait_stream(torch.cuda.current_stream())
+    grads = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, 77, 2, stream=side)
+    side.synchronize()
+    ref.within(O, want, bound, "O")
+    gwant, gbounds = ref.gradient(Q, K, V, O, lse, dO, 77, 2)
+    for g, w, b in zip(grads, gwant, gbounds):
+        ref.within(g, w, b)
+    out = torch.empty_like(Q)
+    s = torch.cuda.current_stream().cuda_stream
+    assert lib.cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), 0, 2, 4, 2, 300, 300, 64, None, 77, 2, 0, 0, s) == 0
+    assert torch.equal(out.view(torch.int16), O.view(torch.int16))
+
+
+def test_a_captured_step(lib):
+    """Forward and gradient in one graph, replayed on new inputs with eager calls between the replays."""
+    shape = (1, 4, 2, 2, 1500, 128)
+    Q, K, V = operands(*shape, 91)
+    dO = normal(Q.shape, 92)
+    step = lambda: (lambda f: (*f, *lib.recurrence_attention_window_grad(Q, K, V, *f, dO, 700, 4)))(lib.recurrence_attention_window(Q, K, V, 700, 4))  # noqa: E731
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for n in range(4):
+        for t, new in zip((Q, K, V, dO), (*operands(*shape, 100 + 4 * n), normal(Q.shape, 103 + 4 * n))):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in captured]
+        for g, e in zip(got, step()):
+            assert torch.equal(g, e)
