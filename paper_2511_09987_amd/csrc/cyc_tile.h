@@ -1,0 +1,100 @@
+// cyc_tile.h -- device helpers shared by the attention kernels: copies into LDS, reads from it that are waited for one by one,
+// reductions over the four lanes of a query, and the layout of a tile of rows.
+#pragma once
+#include "cyc_internal.h"
+
+namespace cyc {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+#define CYC_LDS __attribute__((address_space(3)))
+
+// 64 lanes x 16 bytes from global memory, an address per lane, into LDS at lds_addr + lane * 16
+__device__ __forceinline__ void copy16_from(const char *src, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(src) : "memory", "m0");
+}
+
+__device__ __forceinline__ i32x4 mfma_frag(i32x2 lo, i32x2 hi) { return (i32x4){lo[0], lo[1], hi[0], hi[1]}; }
+__device__ __forceinline__ f32x4 mfma16(i32x4 a, i32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+template <int... I, class F> __device__ __forceinline__ void static_for_each(std::integer_sequence<int, I...>, F &&f)
+{
+    (f(std::integral_constant<int, I>{}), ...);
+}
+// f(integral_constant<int, 0>) .. f(integral_constant<int, N-1>): a loop whose index is a constant expression
+template <int N, class F> __device__ __forceinline__ void static_for(F &&f) { static_for_each(std::make_integer_sequence<int, N>{}, f); }
+
+// 16 bytes per lane from LDS address addr + OFF, with no wait: dst is valid only after lds_wait
+template <int OFF> __device__ __forceinline__ void lds_read128(i32x4 &dst, uint32_t addr)
+{
+    static_assert(OFF >= 0 && OFF < 65536, "the offset field of an LDS instruction has 16 bits");
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF));
+}
+// wait until at most PENDING LDS operations issued after the read of x are outstanding; x is valid from here on
+template <int PENDING> __device__ __forceinline__ void lds_wait(i32x4 &x) { asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(x) : "n"(PENDING)); }
+// the transposing read of four 16-bit elements per lane, likewise without a wait
+template <int OFF> __device__ __forceinline__ void lds_read_tr64(i32x2 &dst, uint32_t addr)
+{
+    static_assert(OFF >= 0 && OFF < 65536, "the offset field of an LDS instruction has 16 bits");
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(dst) : "v"(addr), "n"(OFF));
+}
+template <int PENDING> __device__ __forceinline__ void lds_wait2(i32x2 &x, i32x2 &y) { asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(x), "+v"(y) : "n"(PENDING)); }
+
+// this wave's copies have landed and its LDS reads have returned (the stages it read are about to be requested into
+// again by other waves); then meet the other waves
+__device__ __forceinline__ void landed_barrier() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// f over the values of lanes l, l^16, l^32, l^48.  The swaps exchange halves (rows 2,3 of the first operand with rows 0,1 of the
+// second) resp. odd rows of the first with even rows of the second; fed the same value twice, the two results together
+// hold the value of both partners.  (Elements are copied to scalars before the bit cast: a bit cast applied to a
+// vector element directly reads element 0 whatever the index.)
+template <class F> __device__ __forceinline__ float over_query(float x, F &&f)
+{
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned a0 = a[0], a1 = a[1];
+    const unsigned v = __builtin_bit_cast(unsigned, f(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
+    const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    const unsigned b0 = b[0], b1 = b[1];
+    return f(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
+}
+__device__ __forceinline__ float query_max(float x) { return over_query(x, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
+__device__ __forceinline__ float query_sum(float x) { return over_query(x, [](float a, float b) { return a + b; }); }
+
+// both halves of a packed pair that are finite, the others 0; the signs of infinities and NaNs as +1 / -1 in `up` and `down`
+// (a NaN in both)
+__device__ __forceinline__ int finite_pair(int pair, int &up, int &down)
+{
+    int clean = 0;
+    up = down = 0;
+#pragma unroll
+    for (int s = 0; s < 32; s += 16) {
+        const unsigned h = ((unsigned)pair >> s) & 0xffff, mag = h & 0x7fff;
+        if (mag < 0x7f80) clean |= (int)(h << s);
+        else {
+            if (mag > 0x7f80 || !(h & 0x8000)) up |= 0x3f80 << s;
+            if (mag > 0x7f80 || (h & 0x8000)) down |= 0x3f80 << s;
+        }
+    }
+    return clean;
+}
+
+// What infinities and NaNs of the counted kinds add to a sum of finite terms.
+__device__ __forceinline__ float with_infinities(float sum, float ups, float downs)
+{
+    const float inf = __builtin_inff();
+    return sum + (ups > 0 ? inf : 0.0f) + (downs > 0 ? -inf : 0.0f);
+}
+
+}  // namespace cyc

@@ -2,115 +2,641 @@
 //
 //     O_i = sum_j exp(S_ij - lse_i) V_j,   S_ij = Q_i.K_j / sqrt(d),   lse_i = log sum_j exp S_ij   over the keys j that i sees.
 //
-// One wave per query and head: it walks the visible keys with a running maximum m, sum l and output o,
-//     mh = max(m, S),  l <- exp(m - mh) l + exp(S - mh),  o <- exp(m - mh) o + exp(S - mh) V_j,
-// its lanes sharing the d elements of a row.
+// A row is a (query, head) pair of one key head, row r = query r / group, head r % group of the group: heads that share keys
+// share their tiles too, and one new token fills a wave as far as its group goes.  A workgroup takes a tile of rows and walks the
+// tiles of keys that any of them sees, first those of the sinks, then those of the window, with a running maximum, sum and output per
+// row (cyc_attn.hip has the recurrence and the operand layouts, which are the same here: S^T = K Q^T with the rows stationary in registers,
+// O^T = V^T P^T).  A wave skips the tiles that none of its rows sees and masks only those that some row sees in part.
+// Rows see different keys, so what must not reach a row is kept out twice: a masked score becomes -inf, its weight 0; and since 0 times
+// an infinity or NaN in V would still spoil the sum, a masked tile whose values are not all finite is multiplied without those,
+// which then go to the rows that see them (careful_values).  Keys that no row of the workgroup sees are not read at all: rows
+// of a tile outside [0, sinks) and the window's span are copied from a key inside.
 #include "cyc_window.h"
+#include "cyc_tile.h"
 
+#include <algorithm>
 #include <climits>
 
 namespace cyc {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float x)
+struct TileProblem {
+    const char *Q, *K, *V;
+    char *O;
+    float *lse;
+    int64_t q_batch, q_head, q_row, o_batch, o_head, o_row;         // bytes
+    int64_t k_batch, k_head, k_row, v_batch, v_head, v_row;
+    int64_t page_bytes, table_stride;
+    const int *table, *lengths, *starts;
+    int batch, kv_heads, group, N, M;                                // paged: batch = sequences, N and M by sequence
+    int tiles;                                                       // tiles of rows (paged, long sequences: of all of them together)
+    int tokens, pages, page_shift, max_pages, max_new, short_rows;
+    int window, sinks, splits, part_splits;
+    float scale_log2e;
+    float *part, *refs;                                              // runs of keys: part[run][row][d], refs[run][row][2]
+    int64_t rows;                                                    // of all problems together
+};
+
+enum Addressing { DENSE, PAGED_SHORT, PAGED_LONG };
+
+// First tile slot of sequence b among those of all sequences: sequence b has the slots from here to that of b + 1, at least as many as
+// it has tiles of `per` rows, whatever starts holds.
+__device__ __forceinline__ int first_slot(int start, int group, int per, int b) { return start * group / per + b; }
+
+// Sequence of a slot: one load and ballot for 64 sequences instead of a chain of loads.
+__device__ __forceinline__ int sequence_of_slot(const int *starts, int seqs, int tokens, int group, int per, int slot)
 {
-#pragma unroll
-    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
-    return x;
+    int count = 0;
+    for (int b0 = 0; b0 < seqs; b0 += 64) {
+        const int b = b0 + (threadIdx.x & 63);
+        int at = b < seqs ? starts[b] : 0;
+        at = at < 0 ? 0 : at > tokens ? tokens : at;
+        count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(b < seqs && first_slot(at, group, per, b) <= slot));
+    }
+    return count > 0 ? count - 1 : 0;
 }
 
-// fetch(j, &k, &v): the addresses of key j's rows, or false where there is none that may be read
-template <int D, class Fetch>
-__device__ __forceinline__ void walk(const char *q, char *o, float *lse, int position, int window, int sinks, bool bad, Fetch &&fetch)
+// D: head dimension; KT: keys per tile; NWAVE waves of QB * 16 rows.
+template <int D, int KT, int NWAVE, int QB, Addressing A>
+__global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p)
 {
-    constexpr int E = D / 64;
-    const int l = threadIdx.x & 63;
-    float qv[E], acc[E], m = -__builtin_inff(), sum = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        qv[e] = (float)((const __bf16 *)q)[l * E + e] * (1.0f / __builtin_sqrtf((float)D));
-        acc[e] = 0;
+    constexpr int QW = QB * 16, ROWS = NWAVE * QW;
+    constexpr int KB = KT / 16;           // 16-key blocks per tile
+    constexpr int ROW = D * 2;            // bytes per row
+    constexpr int CPR = ROW / 16;         // 16-byte chunks per row: 16 (D = 128) or 8 (D = 64)
+    constexpr int RPC = 64 / CPR;         // rows per 1 KiB copy
+    constexpr int DS = D / 32;            // MFMA k-steps over d
+    constexpr int DT = D / 16;            // 16-wide d tiles of the output
+    constexpr int TILE_BYTES = KT * ROW;
+    constexpr int COPIES = TILE_BYTES / 1024 / NWAVE;
+    constexpr bool PAGED = A != DENSE;
+    // LDS: two stages of the K tile, then two of the V tile; chunk c of row r sits in slot c ^ swzK(r) resp. c ^ swzV(r), so that
+    // the rows that one operand read touches fall on distinct banks
+    __shared__ __attribute__((aligned(1024))) char lds_raw[4 * TILE_BYTES];
+    CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    auto swzK = [](int r) { return CPR == 16 ? (r & 15) : ((r >> 1) & 7); };
+    auto swzV = [](int r) { return CPR == 16 ? ((r & 7) << 1) : (((r >> 1) & 3) << 1); };
+
+    const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4;
+    const int w = NWAVE == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // Workgroups go to the eight XCDs round robin by their linear index; renumbered, XCD x takes a contiguous range, so that
+    // the tiles of rows that read the same keys run behind one L2.
+    const int total = gridDim.x, xcd = blockIdx.x & 7;
+    int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+    const int splits = p.splits, run = at % splits;
+    at /= splits;
+    int b, head, tile, N = p.N, M = p.M, first = 0;      // problem, key head, tile of rows; queries, keys, first token
+    bool bad = false;
+    if constexpr (A == DENSE) {
+        // tiles with the most keys first, the shortest last, when few workgroups are left to run beside them
+        tile = p.tiles - 1 - at % p.tiles;
+        head = at / p.tiles % p.kv_heads;
+        b = at / p.tiles / p.kv_heads;
+    } else {
+        if constexpr (A == PAGED_SHORT) {
+            b = at / p.kv_heads;
+            head = at % p.kv_heads;
+            tile = 0;
+        } else {
+            const int slot = at % p.tiles;
+            head = at / p.tiles;
+            b = __builtin_amdgcn_readfirstlane(sequence_of_slot(p.starts, p.batch, p.tokens, p.group, ROWS, slot));
+            const int start = p.starts[b];
+            tile = slot - first_slot(start < 0 ? 0 : start > p.tokens ? p.tokens : start, p.group, ROWS, b);
+        }
+        int start = p.starts[b], end = p.starts[b + 1];
+        M = p.lengths[b];
+        bad = start < 0 || end > p.tokens || end < start || M < 0 || M > ((int64_t)p.max_pages << p.page_shift);
+        first = start < 0 ? 0 : start > p.tokens ? p.tokens : start;
+        end = end < first ? first : end > p.tokens ? p.tokens : end;
+        N = end - first;
+        if (N > p.max_new) bad = true;
+        if (bad) M = 0;
+        if (N == 0) return;
+        if constexpr (A == PAGED_SHORT) {
+            // longer sequences have a launch of their own, unless the caller had announced that there are none
+            if ((int64_t)N * p.group > ROWS) {
+                if (N <= p.max_new || run > 0) return;
+                for (int64_t x = l; x < (int64_t)N * p.group * (D / 8); x += 64) {
+                    const int64_t r = x / (D / 8);
+                    char *o = p.O + (first + r / p.group) * p.o_row + (head * p.group + r % p.group) * p.o_head;
+                    *(i32x4 *)(o + x % (D / 8) * 16) = (i32x4){0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0, 0x7fc07fc0};
+                }
+                return;
+            }
+        } else {
+            if (N * p.group <= p.short_rows || tile < 0 || (int64_t)tile * ROWS >= (int64_t)N * p.group) return;
+        }
     }
-    const int lo = position - window + 1;                      // (window INT_MAX: below zero)
-    for (int j = 0; j <= position && !bad; ++j) {
-        if (j >= sinks && j < lo) {
-            j = lo - 1;
-            continue;
-        }
-        const char *k, *v;
-        if (!fetch(j, &k, &v)) {
-            bad = true;
-            break;
-        }
-        float s = 0;
+    const int group = p.group, R = N * group, window = p.window, sinks = p.sinks, pages = p.pages, page_shift = p.page_shift;
+    const int64_t k_row = p.k_row, v_row = p.v_row, page_bytes = p.page_bytes;
+    const int *table = p.table + b * p.table_stride;
+    const float scale_log2e = p.scale_log2e;
+    const char *Q = p.Q + b * (PAGED ? 0 : p.q_batch) + (int64_t)head * group * p.q_head + (int64_t)first * p.q_row;
+    char *O = p.O + b * (PAGED ? 0 : p.o_batch) + (int64_t)head * group * p.o_head + (int64_t)first * p.o_row;
+    const char *K = p.K + (PAGED ? 0 : b * p.k_batch) + (int64_t)head * p.k_head, *V = p.V + (PAGED ? 0 : b * p.v_batch) + (int64_t)head * p.v_head;
+
+    // ---- the keys that the rows of the workgroup see: [0, sink_end) and [lo, hi], as tiles 0 .. sink_tiles - 1 and from
+    // window_tile on; row r stands at position r / group + M - N
+    const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
+    const int p_first = row_first / group + M - N, hi = row_last / group + M - N;
+    const int lo = p_first >= window ? p_first - window + 1 : 0;
+    const int sink_end = sinks < lo ? sinks : lo;
+    const int sink_tiles = (sink_end + KT - 1) / KT, window_tile = lo / KT > sink_tiles ? lo / KT : sink_tiles;
+    const int all_tiles = hi < 0 ? 0 : sink_tiles + (hi / KT - window_tile + 1 > 0 ? hi / KT - window_tile + 1 : 0);
+    const int u_first = (int)((int64_t)all_tiles * run / splits), ntiles = (int)((int64_t)all_tiles * (run + 1) / splits) - u_first;
+    auto tile_key = [&](int u) __attribute__((always_inline)) { return (u + u_first < sink_tiles ? u + u_first : window_tile - sink_tiles + u + u_first) * KT; };
+    // a key that some row sees in place of one that none does
+    auto seen_key = [&](int key) __attribute__((always_inline)) {
+        key = key < hi ? key : hi;
+        return key >= sink_end && key < lo ? lo : key;
+    };
+
+    // ---- this wave's rows: first and last position, and per lane what its rows (one per 16-row block) see
+    const int r0 = row_first + w * QW;
+    const bool idle = r0 > row_last;                      // uniform: a wave without rows helps to copy
+    const int p_lo = idle ? 0 : __builtin_amdgcn_readfirstlane(r0 / group + M - N);
+    const int r_last = r0 + QW - 1 < row_last ? r0 + QW - 1 : row_last;
+    const int p_hi = idle ? -1 : __builtin_amdgcn_readfirstlane(r_last / group + M - N);
+    int row_hi[QB], row_lo[QB];
+    i32x4 qf[QB][DS];
 #pragma unroll
-        for (int e = 0; e < E; ++e) s = __builtin_fmaf(qv[e], (float)((const __bf16 *)k)[l * E + e], s);
-        s = wave_sum(s);
-        const float mh = __builtin_fmaxf(m, s), keep = m == mh ? 1.0f : expf(m - mh), w = expf(s - mh);
-        sum = sum * keep + w;
+    for (int jq = 0; jq < QB; ++jq) {
+        int r = r0 + jq * 16 + lq;
+        r = r < row_last ? r : row_last;                  // rows past the last repeat it and are not stored
+        const int i = r / group, h = r - i * group;
+        row_hi[jq] = i + M - N;
+        row_lo[jq] = (row_hi[jq] < 0 ? 0 : row_hi[jq]) - window + 1;
+        const char *q = Q + i * p.q_row + h * p.q_head + g * 16;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = acc[e] * keep + w * (float)((const __bf16 *)v)[l * E + e];
-        m = mh;
+        for (int ks = 0; ks < DS; ++ks) qf[jq][ks] = *(const i32x4 *)(q + ks * 64);
+    }
+    // ---- copies of a tile of K and V into a stage.  Copy x of wave w moves rows x*NWAVE*RPC + w*RPC .. of the tile, lane l 16 bytes of row
+    // l / CPR of those.  Paged: every lane looks up the pages of its rows a step before it needs them.
+    const int row0 = w * RPC + l / CPR;
+    int entry[COPIES];
+    auto look_up = [&](int u) __attribute__((always_inline)) {
+        const int k0 = tile_key(u);
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) entry[x] = table[seen_key(k0 + x * (NWAVE * RPC) + row0) >> page_shift];
+    };
+    auto issue = [&](int u) __attribute__((always_inline)) {
+        const int k0 = tile_key(u);
+        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES + w * 1024;
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) {
+            const int r = x * (NWAVE * RPC) + row0, key = seen_key(k0 + r);
+            int64_t k_off = key * k_row, v_off = key * v_row;
+            if constexpr (PAGED) {
+                const bool outside = (unsigned)entry[x] >= (unsigned)pages;
+                bad |= outside;
+                k_off = v_off = (outside ? 0 : entry[x]) * page_bytes + (key & ((1 << page_shift) - 1)) * k_row;
+            }
+            copy16_from(K + k_off + (((l % CPR) ^ swzK(r)) << 4), dst + x * (NWAVE * 1024));
+            copy16_from(V + v_off + (((l % CPR) ^ swzV(r)) << 4), dst + 2 * TILE_BYTES + x * (NWAVE * 1024));
+        }
+    };
+
+    // ---- running state of this lane's rows: reference in the log2 domain, this lane's share of the sum, O^T accumulators
+    float m2[QB], sum[QB], tile_sum[QB];
+    f32x4 acc_o[DT][QB];
+#pragma unroll
+    for (int jq = 0; jq < QB; ++jq) {
+        m2[jq] = -__builtin_inff();
+        sum[jq] = 0;
+#pragma unroll
+        for (int id = 0; id < DT; ++id) acc_o[id][jq] = (f32x4){0, 0, 0, 0};
+    }
+    f32x4 s[KB][QB];                                      // S^T: [key block][row block]
+    i32x4 pf[QB][KB / 2];                                 // P^T as B operand: [row block][32-key step]
+
+    // ---- S^T = K_tile Q^T.  Fragment i = ks * KB + ik (16 keys x 32 d) feeds the QB MFMAs of key block ik and d step ks; its read is issued
+    // KWIN fragments ahead of its use and waited for on its own.  The addresses change stage from tile to tile.
+    constexpr int KWIN = 4;
+    constexpr int NFRAG = DS * KB;
+    uint32_t kaddr[DS];
+#pragma unroll
+    for (int ks = 0; ks < DS; ++ks) kaddr[ks] = lds_base + lq * ROW + (((ks * 4 + g) ^ swzK(lq)) << 4);
+    auto scores = [&]() __attribute__((always_inline)) {
+        i32x4 kf[KWIN];
+        static_for<KWIN>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            lds_read128<(i % KB) * 16 * ROW>(kf[i], kaddr[i / KB]);
+        });
+#pragma unroll
+        for (int ik = 0; ik < KB; ++ik)
+#pragma unroll
+            for (int jq = 0; jq < QB; ++jq) s[ik][jq] = (f32x4){0, 0, 0, 0};
+        static_for<NFRAG>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, ks = i / KB, ik = i % KB;
+            constexpr int later = NFRAG - 1 - i < KWIN - 1 ? NFRAG - 1 - i : KWIN - 1;   // reads issued after fragment i
+            lds_wait<later>(kf[i % KWIN]);
+#pragma unroll
+            for (int jq = 0; jq < QB; ++jq) s[ik][jq] = mfma16(kf[i % KWIN], qf[jq][ks], s[ik][jq]);
+            if constexpr (i + KWIN < NFRAG) lds_read128<((i + KWIN) % KB) * 16 * ROW>(kf[i % KWIN], kaddr[(i + KWIN) / KB]);
+        });
+    };
+
+    // ---- O^T += V^T P^T.  A operand lane: d = 16 id + l%16; k-slots 0..3 = keys 32 sk + 4 (l/16) .. +3, k-slots 4..7 = the same keys of
+    // the next 16-key block (the order P^T is packed in); two transposing reads, issued VWIN fragments ahead.
+    constexpr int VWIN = 4;
+    constexpr int NVFRAG = (KB / 2) * DT;
+    uint32_t vaddr[DT];
+#pragma unroll
+    for (int id = 0; id < DT; ++id) {
+        const int row = 4 * g + (lq >> 2);
+        const int chunk = (id * 16 + 4 * (lq & 3)) >> 3, within = ((id * 16 + 4 * (lq & 3)) & 7) * 2;
+        vaddr[id] = lds_base + 2 * TILE_BYTES + row * ROW + ((chunk ^ swzV(row)) << 4) + within;
+    }
+    auto weighted_values = [&]() __attribute__((always_inline)) {
+        i32x2 first_half[VWIN], second_half[VWIN];
+        static_for<VWIN>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, off = (i / DT) * 32 * ROW;
+            lds_read_tr64<off>(first_half[i], vaddr[i % DT]);
+            lds_read_tr64<off + 16 * ROW>(second_half[i], vaddr[i % DT]);
+        });
+        static_for<NVFRAG>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, sk = i / DT, id = i % DT;
+            constexpr int later = NVFRAG - 1 - i < VWIN - 1 ? NVFRAG - 1 - i : VWIN - 1;   // fragments requested after i
+            lds_wait2<2 * later>(first_half[i % VWIN], second_half[i % VWIN]);
+            const i32x4 vf = mfma_frag(first_half[i % VWIN], second_half[i % VWIN]);
+#pragma unroll
+            for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(vf, pf[jq][sk], acc_o[id][jq]);
+            if constexpr (i + VWIN < NVFRAG) {
+                constexpr int off = ((i + VWIN) / DT) * 32 * ROW;
+                lds_read_tr64<off>(first_half[i % VWIN], vaddr[(i + VWIN) % DT]);
+                lds_read_tr64<off + 16 * ROW>(second_half[i % VWIN], vaddr[(i + VWIN) % DT]);
+            }
+        });
+    };
+
+    // ---- weights against the reference m2 (which follows the running maximum lazily, as in cyc_attn.hip), their sum, and P^T packed
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq) {
+            float part0 = 0, part1 = 0;
+#pragma unroll
+            for (int ik = 0; ik < KB; ++ik)
+#pragma unroll
+                for (int r = 0; r < 4; r += 2) {
+                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ik][jq][r], scale_log2e, -m2[jq]));
+                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ik][jq][r + 1], scale_log2e, -m2[jq]));
+                    part0 += p0;
+                    part1 += p1;
+                    const bf16x2 pair = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+                    pf[jq][ik >> 1][(ik & 1) * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
+                }
+            tile_sum[jq] = part0 + part1;
+        }
+    };
+    constexpr unsigned short LAG_BITS = 0x4380;           // 2^8 as bfloat16
+    auto overflowed = [&]() __attribute__((always_inline)) {
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+            for (int sk = 0; sk < KB / 2; ++sk)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int word = pf[jq][sk][r];
+                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
+                }
+        const unsigned short t0 = top[0], t1 = top[1];
+        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) > LAG_BITS) != 0;
+    };
+    auto rebase = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq) {
+            float top = s[0][jq][0];
+#pragma unroll
+            for (int ik = 0; ik < KB; ++ik)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) top = __builtin_fmaxf(top, s[ik][jq][r]);
+            // (a row that has seen nothing yet keeps a finite reference: weights 0 against it, and any score lifts it)
+            const float mh = __builtin_fmaxf(__builtin_fmaxf(m2[jq], query_max(top) * scale_log2e), -3.0e38f);
+            const float keep = __builtin_amdgcn_exp2f(m2[jq] - mh);
+            m2[jq] = mh;
+            sum[jq] *= keep;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) acc_o[id][jq] *= keep;
+        }
+    };
+
+    // ---- tiles that some row sees in part
+    auto visible = [&](int key, int jq) __attribute__((always_inline)) { return key <= row_hi[jq] && (key >= row_lo[jq] || key < sinks); };
+    auto mask = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+            for (int ik = 0; ik < KB; ++ik)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s[ik][jq][r] = visible(k0 + 4 * g + ik * 16 + r, jq) ? s[ik][jq][r] : -__builtin_inff();
+    };
+    // is there an infinity or NaN among the tile's values?
+    auto any_infinite = [&](int stage) __attribute__((always_inline)) {
+        const CYC_LDS i32x4 *v = (const CYC_LDS i32x4 *)(lds + (2 + stage) * TILE_BYTES) + l;
+        u16x2 top = {0, 0};
+#pragma unroll 4
+        for (int x = 0; x < TILE_BYTES / 1024; ++x) {
+            const i32x4 four = v[x * 64];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int word = four[r] & 0x7fff7fff;
+                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
+            }
+        }
+        const unsigned short t0 = top[0], t1 = top[1];
+        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) >= 0x7f80) != 0;
+    };
+    // O^T += V^T P^T with the finite values, and infinities and NaNs to the rows that see them: products with ones count those
+    auto careful_values = [&](int k0) __attribute__((always_inline)) {
+#pragma unroll
+        for (int id = 0; id < DT; ++id)
+#pragma unroll
+            for (int jq = 0; jq < QB; ++jq) {
+                f32x4 ups = {0, 0, 0, 0}, downs = {0, 0, 0, 0};
+                int here = k0 + 4 * g;
+                asm("" : "+v"(here));                     // (keeps the masks from being held in registers for all of them)
+#pragma unroll
+                for (int sk = 0; sk < KB / 2; ++sk) {
+                    i32x2 a, c;
+                    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                                 : "=&v"(a), "=&v"(c) : "v"(vaddr[id]), "n"(sk * 32 * ROW), "n"((sk * 32 + 16) * ROW));
+                    i32x4 clean, up, down, ones;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        int u1, d1;
+                        const int word = x < 2 ? a[x & 1] : c[x & 1], key = here + sk * 32 + (x >> 1) * 16 + (x & 1) * 2;
+                        clean[x] = finite_pair(word, u1, d1);
+                        up[x] = u1;
+                        down[x] = d1;
+                        ones[x] = (visible(key, jq) ? 0x3f80 : 0) | (visible(key + 1, jq) ? 0x3f800000 : 0);
+                    }
+                    acc_o[id][jq] = mfma16(clean, pf[jq][sk], acc_o[id][jq]);
+                    ups = mfma16(up, ones, ups);
+                    downs = mfma16(down, ones, downs);
+                }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) acc_o[id][jq][r] = with_infinities(acc_o[id][jq][r], ups[r], downs[r]);
+            }
+    };
+
+    // ---- One barrier per tile: tile u has landed and every wave is done with tile u-1, whose stage tile u+1 is then requested into.
+    // What a wave's tile needs it tells by scalar arithmetic.  The other workgroup on the compute unit fills the gaps between the matrix
+    // products and the vector work of a tile.
+    if (ntiles > 0) {
+        if constexpr (PAGED) look_up(0);
+        issue(0);
+        if constexpr (PAGED) {
+            if (ntiles > 1) look_up(1);
+        }
+    }
+    for (int u = 0; u < ntiles; ++u) {
+        landed_barrier();
+        if (u + 1 < ntiles) {
+            issue(u + 1);
+            if constexpr (PAGED) {
+                if (u + 2 < ntiles) look_up(u + 2);
+            }
+        }
+        const int k0 = tile_key(u), k1 = k0 + KT - 1;
+        const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
+        if (!none) {
+            const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
+            bool careful = false;
+            scores();
+            if (!all) {
+                mask(k0);
+                careful = any_infinite(u & 1);
+            }
+            weights();
+            if (__builtin_expect(overflowed(), 0)) {
+                rebase();
+                weights();
+            }
+#pragma unroll
+            for (int jq = 0; jq < QB; ++jq) sum[jq] += tile_sum[jq];
+            if (__builtin_expect(careful, 0)) careful_values(k0);
+            else weighted_values();
+        }
+        // the other stage
+        const int turn = u & 1 ? -TILE_BYTES : TILE_BYTES;
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) kaddr[ks] += turn;
+#pragma unroll
+        for (int id = 0; id < DT; ++id) vaddr[id] += turn;
+    }
+
+    if constexpr (PAGED) {
+        // a lane of any wave may have met a table entry that is none: the whole tile of rows is in doubt
+        bool any = __builtin_amdgcn_ballot_w64(bad) != 0;
+        if constexpr (NWAVE > 1) {
+            landed_barrier();
+            if (l == 0) ((CYC_LDS int *)lds)[w] = any;
+            landed_barrier();
+#pragma unroll
+            for (int x = 0; x < NWAVE; ++x) any |= ((CYC_LDS int *)lds)[x] != 0;
+        }
+        bad = any;
+    }
+    // ---- O = o / sum.  Accumulator register r of lane l: d = 16 id + 4 (l/16) + r, row 16 jq + l%16.
+#pragma unroll
+    for (int jq = 0; jq < QB; ++jq) {
+        const int r = r0 + jq * 16 + lq;
+        const float tot = bad ? __builtin_nanf("") : query_sum(sum[jq]);
+        if (r > row_last) continue;
+        const int i = r / group, h = head * group + r - i * group;
+        if (splits > 1) {
+            const int64_t row = PAGED ? (int64_t)(first + i) * (p.kv_heads * group) + h : ((int64_t)b * (p.kv_heads * group) + h) * N + i;
+            const int64_t slot = run * p.rows + row;
+            if (ntiles > 0)
+#pragma unroll
+                for (int id = 0; id < DT; ++id) *(f32x4 *)(p.part + slot * D + id * 16 + 4 * g) = acc_o[id][jq];
+            if (g == 0) *(f32x2 *)(p.refs + slot * 2) = (f32x2){m2[jq], tot};
+        } else {
+            const bool empty = row_hi[jq] < 0 && !bad;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) {
+                bf16x4 o;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) o[x] = (__bf16)(empty ? 0.0f : acc_o[id][jq][x] / tot);
+                *(bf16x4 *)(O + i * p.o_row + (r - i * group) * p.o_head + (id * 16 + 4 * g) * 2) = o;
+            }
+            if (!PAGED && p.lse && g == 0)
+                p.lse[((int64_t)b * (p.kv_heads * group) + h) * N + i] = empty ? -__builtin_inff() : (m2[jq] + __builtin_amdgcn_logf(tot)) * 0.69314718055994531f;
+        }
+    }
+}
+
+// Joins the runs of a row in ascending order: O = sum_x exp(m_x - m) o_x / sum_x exp(m_x - m) l_x, m the largest m_x.  One thread per four
+// d; bound by a launch and the reads of part.  A run without tiles has m_x = -inf and l_x = 0, and no o_x.
+template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(const TileProblem p, int short_splits, int long_splits)
+{
+    const int64_t row = (int64_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
+    const int c = threadIdx.x % (D / 4) * 4, heads = p.kv_heads * p.group;
+    if (row >= p.rows) return;
+    int h, i, position, splits = long_splits;
+    int64_t b = 0;
+    if constexpr (PAGED) {
+        i = (int)(row / heads);
+        h = (int)(row % heads);
+        const int seq = sequence_of(p.starts, p.batch, i), start = p.starts[seq], end = p.starts[seq + 1], n = end - start;
+        if (i < start || i >= end) return;
+        if ((int64_t)n * p.group <= p.short_rows) splits = short_splits;
+        else if (p.tiles == 0) return;                                // (no launch for it: its rows are NaN already)
+        position = p.lengths[seq] - end + i;
+        if (start < 0 || end > p.tokens || n > p.max_new || p.lengths[seq] < 0) position = 0;
+    } else {
+        i = (int)(row % p.N);
+        h = (int)(row / p.N % heads);
+        b = row / p.N / heads;
+        position = i + p.M - p.N;
+    }
+    if (splits <= 1) return;
+    const float *ref = p.refs + row * 2, *part = p.part + row * D + c;
+    float m = -__builtin_inff();
+    for (int x = 0; x < splits; ++x) m = __builtin_fmaxf(m, ref[x * p.rows * 2]);
+    f32x4 o = {0, 0, 0, 0};
+    float tot = 0;
+#pragma unroll 4
+    for (int x = 0; x < splits; ++x) {
+        const f32x2 mt = *(const f32x2 *)(ref + x * p.rows * 2);
+        if (mt[0] == -__builtin_inff() && mt[1] == 0) continue;
+        const float keep = mt[0] == m ? 1.0f : __builtin_amdgcn_exp2f(mt[0] - m);
+        tot = __builtin_fmaf(keep, mt[1], tot);
+        const f32x4 v = *(const f32x4 *)(part + x * p.rows * D);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) o[y] = __builtin_fmaf(keep, v[y], o[y]);
     }
     const bool empty = position < 0;
+    bf16x4 out;
 #pragma unroll
-    for (int e = 0; e < E; ++e) ((__bf16 *)o)[l * E + e] = (__bf16)(bad ? __builtin_nanf("") : empty ? 0.0f : acc[e] / sum);
-    if (lse && l == 0) *lse = empty ? -__builtin_inff() : m + logf(sum);
+    for (int y = 0; y < 4; ++y) out[y] = (__bf16)(empty ? 0.0f : o[y] / tot);
+    *(bf16x4 *)(p.O + b * p.o_batch + h * p.o_head + i * p.o_row + c * 2) = out;
+    if (!PAGED && p.lse && c == 0) p.lse[row] = empty ? -__builtin_inff() : (m + __builtin_amdgcn_logf(tot)) * 0.69314718055994531f;
 }
 
-template <int D> __global__ __launch_bounds__(256) void window_kernel(WindowProblem p)
+constexpr int LONG_ROWS = 128, SHORT_ROWS = 16;
+template <int D> constexpr int LONG_KEYS = 8192 / D;
+template <int D> constexpr int SHORT_KEYS = 4096 / D;
+
+// Runs of keys for `groups` workgroups that walk up to `keys` keys each, in tiles of kt: enough to fill the chip's slots once, tiles
+// enough in each to pay for starting it.
+int choose_splits(int64_t groups, int64_t keys, int64_t kt, int64_t slots, int64_t rows, int64_t d)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)p.batch * p.heads * p.N) return;
-    const int i = (int)(row % p.N), h = (int)(row / p.N % p.heads);
-    const int64_t b = row / p.N / p.heads;
-    const char *K = p.K.base + b * p.K.batch + h / p.group * p.K.head, *V = p.V.base + b * p.V.batch + h / p.group * p.V.head;
-    walk<D>(p.Q.base + b * p.Q.batch + h * p.Q.head + i * p.Q.row, (char *)p.O.base + b * p.O.batch + h * p.O.head + i * p.O.row,
-            p.lse ? p.lse + row : nullptr, i + p.M - p.N, p.window, p.sinks, false, [&](int j, const char **k, const char **v) {
-                *k = K + j * p.K.row;
-                *v = V + j * p.V.row;
-                return true;
-            });
+    int64_t splits = std::min(slots / std::max<int64_t>(groups, 1), (keys + kt - 1) / kt / 4);
+    splits = std::min<int64_t>(splits, (64 << 20) / (rows * (d + 2) * 4));
+    return (int)std::max<int64_t>(std::min<int64_t>(splits, 64), 1);
 }
 
-template <int D> __global__ __launch_bounds__(256) void paged_kernel(PagedProblem p)
+// keys that a row can see at most
+int64_t most_keys(int64_t keys, int window, int sinks, int64_t queries)
 {
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)p.tokens * p.heads) return;
-    const int t = (int)(row / p.heads), h = (int)(row % p.heads), b = sequence_of(p.starts, p.seqs, t);
-    const int first = p.starts[b], end = p.starts[b + 1], n = p.lengths[b];
-    if (t < first || t >= end) return;
-    const bool bad = first < 0 || end > p.tokens || end - first > p.max_new || n < 0 || n > ((int64_t)p.max_pages << p.page_shift);
-    const int *table = p.table + b * p.table_stride;
-    walk<D>(p.Q + t * p.q_token + h * p.q_head, p.O + t * p.o_token + h * p.o_head, nullptr, n - end + t, p.window, p.sinks, bad,
-            [&](int j, const char **k, const char **v) {
-                const int at = table[j >> p.page_shift];
-                if ((unsigned)at >= (unsigned)p.pages) return false;
-                const int64_t off = at * p.page_bytes + h / p.group * p.head_bytes + (j & ((1 << p.page_shift) - 1)) * p.row_bytes;
-                *k = p.K + off;
-                *v = p.V + off;
-                return true;
-            });
+    return std::min<int64_t>(keys, (int64_t)window + sinks + queries);
+}
+
+struct Mapping {
+    int short_splits, long_splits;       // 0: no launch for such sequences
+};
+
+int64_t part_bytes(int64_t rows, int64_t d, int splits) { return splits > 1 ? (rows * splits * (d + 2) * 4 + 15) / 16 * 16 : 0; }
+
+Mapping window_mapping(const WindowProblem &p)
+{
+    const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads;
+    const int64_t keys = most_keys(p.M, p.window, p.sinks, p.N);
+    if (R <= SHORT_ROWS) return {choose_splits(pairs, keys, 4096 / p.d, 1280, R * pairs, p.d), 0};
+    return {0, choose_splits(pairs * ((R + LONG_ROWS - 1) / LONG_ROWS), keys, 8192 / p.d, 512, R * pairs, p.d)};
+}
+
+int64_t long_slots(const PagedProblem &p) { return (int64_t)p.tokens * p.group / LONG_ROWS + p.seqs; }
+
+Mapping paged_mapping(const PagedProblem &p)
+{
+    const int64_t keys = most_keys((int64_t)p.max_pages << p.page_shift, p.window, p.sinks, p.max_new), rows = (int64_t)p.tokens * p.heads;
+    Mapping m = {0, 0};
+    const bool longs = (int64_t)p.max_new * p.group > SHORT_ROWS;
+    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.short_splits = choose_splits((int64_t)p.seqs * p.kv_heads, keys, 4096 / p.d, 1280, rows, p.d);
+    if (longs) m.long_splits = choose_splits(long_slots(p) * p.kv_heads, keys, 8192 / p.d, 512, rows, p.d);
+    return m;
+}
+
+template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, const Mapping &m, hipStream_t s)
+{
+    hipError_t e = hipSuccess;
+    auto launch = [&](auto kernel, int threads, int64_t groups, int splits) {
+        t.splits = splits;
+        if (groups * splits >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+        return launch_kernel(kernel, dim3((unsigned)(groups * splits)), dim3(threads), s, t);
+    };
+    if (m.short_splits) {
+        const int64_t groups = (int64_t)t.batch * t.kv_heads;
+        e = launch(tile_kernel<D, SHORT_KEYS<D>, 1, 1, PAGED ? PAGED_SHORT : DENSE>, 64, groups, m.short_splits);
+    }
+    if (e == hipSuccess && m.long_splits)
+        e = launch(tile_kernel<D, LONG_KEYS<D>, 4, 2, PAGED ? PAGED_LONG : DENSE>, 256, (int64_t)t.tiles * t.kv_heads * (PAGED ? 1 : t.batch), m.long_splits);
+    if (e != hipSuccess || std::max(m.short_splits, m.long_splits) <= 1) return e;
+    const int64_t per = 1024 / D;
+    return launch_kernel(join_kernel<D, PAGED>, dim3((unsigned)((t.rows + per - 1) / per)), dim3(256), s, t, m.short_splits, PAGED ? m.long_splits : std::max(m.short_splits, m.long_splits));
+}
+
+void split_memory(TileProblem &t, Mapping &m, int64_t d, void *workspace, int64_t workspace_bytes)
+{
+    const int splits = std::max(m.short_splits, m.long_splits);
+    if (part_bytes(t.rows, d, splits) > workspace_bytes) {
+        m.short_splits = std::min(m.short_splits, 1);
+        m.long_splits = std::min(m.long_splits, 1);
+    }
+    t.part = (float *)workspace;
+    t.refs = t.part + t.rows * d * splits;
+    t.scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
 }
 
 }  // namespace
 
-int64_t window_workspace_bytes(const WindowProblem &) { return 0; }
-
-hipError_t launch_window(const WindowProblem &p, void *, int64_t, hipStream_t s)
+int64_t window_workspace_bytes(const WindowProblem &p)
 {
-    const int64_t rows = (int64_t)p.batch * p.heads * p.N;
-    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
-    return p.d == 128 ? launch_kernel(window_kernel<128>, grid, block, s, p) : launch_kernel(window_kernel<64>, grid, block, s, p);
+    const Mapping m = window_mapping(p);
+    return part_bytes((int64_t)p.batch * p.heads * p.N, p.d, std::max(m.short_splits, m.long_splits));
 }
 
-int64_t paged_workspace_bytes(const PagedProblem &) { return 0; }
-
-hipError_t launch_paged(const PagedProblem &p, void *, int64_t, hipStream_t s)
+hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
 {
-    const int64_t rows = (int64_t)p.tokens * p.heads;
-    const dim3 grid((unsigned)((rows + 3) / 4)), block(256);
-    return p.d == 128 ? launch_kernel(paged_kernel<128>, grid, block, s, p) : launch_kernel(paged_kernel<64>, grid, block, s, p);
+    TileProblem t{};
+    t.Q = p.Q.base, t.K = p.K.base, t.V = p.V.base, t.O = (char *)p.O.base, t.lse = p.lse;
+    t.q_batch = p.Q.batch, t.q_head = p.Q.head, t.q_row = p.Q.row, t.o_batch = p.O.batch, t.o_head = p.O.head, t.o_row = p.O.row;
+    t.k_batch = p.K.batch, t.k_head = p.K.head, t.k_row = p.K.row, t.v_batch = p.V.batch, t.v_head = p.V.head, t.v_row = p.V.row;
+    t.batch = p.batch, t.kv_heads = p.kv_heads, t.group = p.group, t.N = p.N, t.M = p.M;
+    t.window = p.window, t.sinks = p.sinks;
+    t.rows = (int64_t)p.batch * p.heads * p.N;
+    Mapping m = window_mapping(p);
+    t.tiles = m.short_splits ? 1 : (int)(((int64_t)p.N * p.group + LONG_ROWS - 1) / LONG_ROWS);
+    split_memory(t, m, p.d, workspace, workspace_bytes);
+    return p.d == 128 ? launch_tiles<128, false>(t, m, s) : launch_tiles<64, false>(t, m, s);
+}
+
+int64_t paged_workspace_bytes(const PagedProblem &p)
+{
+    const Mapping m = paged_mapping(p);
+    return part_bytes((int64_t)p.tokens * p.heads, p.d, std::max(m.short_splits, m.long_splits));
+}
+
+hipError_t launch_paged(const PagedProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
+{
+    TileProblem t{};
+    t.Q = p.Q, t.K = p.K, t.V = p.V, t.O = p.O;
+    t.q_head = p.q_head, t.q_row = p.q_token, t.o_head = p.o_head, t.o_row = p.o_token;
+    t.k_head = t.v_head = p.head_bytes, t.k_row = t.v_row = p.row_bytes, t.page_bytes = p.page_bytes, t.table_stride = p.table_stride;
+    t.table = p.table, t.lengths = p.lengths, t.starts = p.starts;
+    t.batch = p.seqs, t.kv_heads = p.kv_heads, t.group = p.group, t.tokens = p.tokens, t.pages = p.pages, t.page_shift = p.page_shift;
+    t.max_pages = p.max_pages, t.max_new = p.max_new, t.window = p.window, t.sinks = p.sinks;
+    t.rows = (int64_t)p.tokens * p.heads;
+    Mapping m = paged_mapping(p);
+    t.short_rows = m.short_splits ? SHORT_ROWS : 0;
+    t.tiles = m.long_splits ? (int)long_slots(p) : 0;
+    split_memory(t, m, p.d, workspace, workspace_bytes);
+    return p.d == 128 ? launch_tiles<128, true>(t, m, s) : launch_tiles<64, true>(t, m, s);
 }
 
 }  // namespace cyc

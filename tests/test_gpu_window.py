@@ -233,6 +233,23 @@ def test_refusals_of_device_tensors(lib):
         call(Q, K, V, out=normal((1, 1, 8, 64), 1).expand(1, 2, 8, 64))
 
 
+def test_a_workspace_too_small_counts_as_none(lib):
+    batch, heads, kv, N, M, d = 1, 2, 1, 1, 4000, 128
+    Q, K, V = operands(batch, heads, kv, N, M, d, 71)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, None, 0)
+    wanted = lib.cyc_attention_window_workspace(batch, heads, kv, N, M, d, 0, 0)
+    assert wanted > 0
+    work = torch.full((wanted + 64,), 255, dtype=torch.uint8, device=DEV)
+    for size in (0, wanted - 1, wanted):
+        O, lse = torch.empty_like(Q), torch.empty(Q.shape[:3], device=DEV)
+        s = torch.cuda.current_stream().cuda_stream
+        assert lib.cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), batch, heads, kv, N, M,
+                                                   d, None, 0, 0, work.data_ptr() if size else 0, size, s) == 0
+        ref.within(O, want, bound, "O")
+        ref.within(lse, wlse, lbound, "lse")
+    assert bool((work[wanted:] == 255).all())
+
+
 def test_another_stream_and_no_lse(lib):
     Q, K, V = operands(2, 4, 2, 300, 300, 64, 81)
     want, wlse, bound, lbound = ref.forward(Q, K, V, 77, 2)
