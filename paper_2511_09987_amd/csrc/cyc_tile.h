@@ -72,29 +72,11 @@ template <class F> __device__ __forceinline__ float over_query(float x, F &&f)
 __device__ __forceinline__ float query_max(float x) { return over_query(x, [](float a, float b) { return __builtin_fmaxf(a, b); }); }
 __device__ __forceinline__ float query_sum(float x) { return over_query(x, [](float a, float b) { return a + b; }); }
 
-// both halves of a packed pair that are finite, the others 0; the signs of infinities and NaNs as +1 / -1 in `up` and `down`
-// (a NaN in both)
-__device__ __forceinline__ int finite_pair(int pair, int &up, int &down)
+// a packed pair of bfloat16 with 0 in place of infinities and NaNs
+__device__ __forceinline__ int finite_pair(int pair)
 {
-    int clean = 0;
-    up = down = 0;
-#pragma unroll
-    for (int s = 0; s < 32; s += 16) {
-        const unsigned h = ((unsigned)pair >> s) & 0xffff, mag = h & 0x7fff;
-        if (mag < 0x7f80) clean |= (int)(h << s);
-        else {
-            if (mag > 0x7f80 || !(h & 0x8000)) up |= 0x3f80 << s;
-            if (mag > 0x7f80 || (h & 0x8000)) down |= 0x3f80 << s;
-        }
-    }
-    return clean;
-}
-
-// What infinities and NaNs of the counted kinds add to a sum of finite terms.
-__device__ __forceinline__ float with_infinities(float sum, float ups, float downs)
-{
-    const float inf = __builtin_inff();
-    return sum + (ups > 0 ? inf : 0.0f) + (downs > 0 ? -inf : 0.0f);
+    const unsigned u = (unsigned)pair, low = (u & 0x7f80u) == 0x7f80u ? 0 : u & 0xffffu, high = (u & 0x7f800000u) == 0x7f800000u ? 0 : u & 0xffff0000u;
+    return (int)(low | high);
 }
 
 }  // namespace cyc

@@ -349,37 +349,34 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
         const unsigned short t0 = top[0], t1 = top[1];
         return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) >= 0x7f80) != 0;
     };
-    // O^T += V^T P^T with the finite values, and infinities and NaNs to the rows that see them: products with ones count those
-    auto careful_values = [&](int k0) __attribute__((always_inline)) {
+    // O^T += V^T P^T with the finite values alone, then infinities and NaNs, key by key, to the rows that see them
+    auto careful_values = [&](int k0, int stage) __attribute__((always_inline)) {
 #pragma unroll
-        for (int id = 0; id < DT; ++id)
+        for (int sk = 0; sk < KB / 2; ++sk)
 #pragma unroll
-            for (int jq = 0; jq < QB; ++jq) {
-                f32x4 ups = {0, 0, 0, 0}, downs = {0, 0, 0, 0};
-                int here = k0 + 4 * g;
-                asm("" : "+v"(here));                     // (keeps the masks from being held in registers for all of them)
+            for (int id = 0; id < DT; ++id) {
+                i32x2 a, c;
+                asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
+                             : "=&v"(a), "=&v"(c) : "v"(vaddr[id]), "n"(sk * 32 * ROW), "n"((sk * 32 + 16) * ROW));
+                const i32x4 clean = {finite_pair(a[0]), finite_pair(a[1]), finite_pair(c[0]), finite_pair(c[1])};
 #pragma unroll
-                for (int sk = 0; sk < KB / 2; ++sk) {
-                    i32x2 a, c;
-                    asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
-                                 : "=&v"(a), "=&v"(c) : "v"(vaddr[id]), "n"(sk * 32 * ROW), "n"((sk * 32 + 16) * ROW));
-                    i32x4 clean, up, down, ones;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        int u1, d1;
-                        const int word = x < 2 ? a[x & 1] : c[x & 1], key = here + sk * 32 + (x >> 1) * 16 + (x & 1) * 2;
-                        clean[x] = finite_pair(word, u1, d1);
-                        up[x] = u1;
-                        down[x] = d1;
-                        ones[x] = (visible(key, jq) ? 0x3f80 : 0) | (visible(key + 1, jq) ? 0x3f800000 : 0);
-                    }
-                    acc_o[id][jq] = mfma16(clean, pf[jq][sk], acc_o[id][jq]);
-                    ups = mfma16(up, ones, ups);
-                    downs = mfma16(down, ones, downs);
-                }
-#pragma unroll
-                for (int r = 0; r < 4; ++r) acc_o[id][jq][r] = with_infinities(acc_o[id][jq][r], ups[r], downs[r]);
+                for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(clean, pf[jq][sk], acc_o[id][jq]);
             }
+        for (int key = 0; key < KT; ++key) {
+            const CYC_LDS char *row = lds + (2 + stage) * TILE_BYTES + key * ROW;
+            const int word = ((const CYC_LDS int *)row)[l % (ROW / 4)];
+            if (__builtin_amdgcn_ballot_w64(finite_pair(word) != word) == 0) continue;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) {
+                const int chunk = (id * 16 + 4 * g) >> 3, within = ((id * 16 + 4 * g) & 7) * 2;
+                const bf16x4 v = *(const CYC_LDS bf16x4 *)(row + ((chunk ^ swzV(key)) << 4) + within);
+#pragma unroll
+                for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+                        if (visible(k0 + key, jq) && !__builtin_isfinite((float)v[r])) acc_o[id][jq][r] += (float)v[r];
+            }
+        }
     };
 
     // ---- One barrier per tile: tile u has landed and every wave is done with tile u-1, whose stage tile u+1 is then requested into.
@@ -417,7 +414,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             }
 #pragma unroll
             for (int jq = 0; jq < QB; ++jq) sum[jq] += tile_sum[jq];
-            if (__builtin_expect(careful, 0)) careful_values(k0);
+            if (__builtin_expect(careful, 0)) careful_values(k0, u & 1);
             else weighted_values();
         }
         // the other stage

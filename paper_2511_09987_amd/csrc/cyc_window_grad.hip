@@ -2,105 +2,557 @@
 //
 // With P_ij = exp(S_ij - lse_i) over the keys that i sees, D_i = dO_i.O_i and dS_ij = P_ij (dO_i.V_j - D_i):
 //     dQ_i = sum_j dS_ij K_j / sqrt(d),   dK_j = sum_i dS_ij Q_i / sqrt(d),   dV_j = sum_i P_ij dO_i,
-// the last two also over the heads that share key j.  One wave per query for dQ and one per key for dK and dV, lanes along d.
+// the last two also over the heads that share key j.  Two kernels, so that every sum stays with one owner and no atomic adds are needed:
+// one keeps rows (query, head) and walks their keys for dQ (three products a pair), the other keeps keys and walks the rows that
+// see them for dK and dV (four); P is taken again in the second.  Seven products for the five of the formulas, against the
+// 4 d bytes per pair that P and dS would cost in memory.
+//
+// Rows (resp. keys) stay in MFMA operand registers, as in cyc_window.hip, and the other side streams through LDS in tiles that are read
+// in two ways: row by row (16 bytes of a row per lane) for the products along d, transposed for those along rows or keys.  The
+// accumulators of the first kind, rounded, are operands of the second kind as they are.
+// What a row does not see is kept out as in cyc_window.hip: P and dS are 0 there by selection, and a masked tile that is not all finite
+// is multiplied without what is not, which then goes to those that see it.
 #include "cyc_window.h"
+#include "cyc_tile.h"
+
+#include <algorithm>
+#include <climits>
 
 namespace cyc {
 namespace {
 
-__device__ __forceinline__ float wave_sum(float x)
-{
-#pragma unroll
-    for (int m = 32; m; m >>= 1) x += __shfl_xor(x, m);
-    return x;
-}
+// In a tile of rows of ROW bytes chunk c of row r sits in slot c ^ swizzle(r): the 16 rows that a row-wise read touches fall on
+// distinct banks, and so do the eight rows of half a transposing read.  Linear in the bits of r.
+template <int CPR> __device__ __forceinline__ constexpr int swizzle(int r) { return CPR == 16 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1)); }
 
-template <int E> __device__ __forceinline__ void load(float (&x)[E], const char *row)
-{
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = (float)((const __bf16 *)row)[(threadIdx.x & 63) * E + e];
-}
-template <int E> __device__ __forceinline__ float dot(const float (&x)[E], const float (&y)[E])
-{
-    float s = 0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) s = __builtin_fmaf(x[e], y[e], s);
-    return wave_sum(s);
-}
-template <int E> __device__ __forceinline__ void store(char *row, const float (&x)[E], float scale)
-{
-#pragma unroll
-    for (int e = 0; e < E; ++e) ((__bf16 *)row)[(threadIdx.x & 63) * E + e] = (__bf16)(x[e] * scale);
-}
-__device__ __forceinline__ const char *row_of(const Strided &x, int64_t b, int h, int i) { return x.base + b * x.batch + h * x.head + i * x.row; }
+constexpr int TILE = 32;                 // rows of a tile of queries, keys of a step
 
-template <int D> __global__ __launch_bounds__(256) void grad_q_kernel(WindowProblem p, float *Ds)
-{
-    constexpr int E = D / 64;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)p.batch * p.heads * p.N) return;
-    const int i = (int)(row % p.N), h = (int)(row / p.N % p.heads), position = i + p.M - p.N, g = h / p.group;
-    const int64_t b = row / p.N / p.heads;
-    const float scale = 1.0f / __builtin_sqrtf((float)D);
-    float q[E], o[E], dO[E], k[E], v[E], dq[E] = {};
-    load(q, row_of(p.Q, b, h, i));
-    load(o, row_of(p.O, b, h, i));
-    load(dO, row_of(p.dO, b, h, i));
-    const float Di = dot(o, dO), lse = p.lse[row];
-    if ((threadIdx.x & 63) == 0) Ds[row] = Di;
-    for (int j = 0; j <= position; ++j) {
-        if (!sees(position, j, p.window, p.sinks)) continue;
-        load(k, row_of(p.K, b, g, j));
-        load(v, row_of(p.V, b, g, j));
-        const float w = expf(dot(q, k) * scale - lse) * (dot(dO, v) - Di);
-#pragma unroll
-        for (int e = 0; e < E; ++e) dq[e] = __builtin_fmaf(w, k[e], dq[e]);
+// What both kernels do with a tile of 32 rows in LDS.  D: head dimension.
+template <int D> struct Tile {
+    static constexpr int ROW = D * 2, CPR = ROW / 16, DS = D / 32, DT = D / 16, WIN = 4;
+    // this lane's addresses within a tile: row l % 16 (chunk l / 16 of 64 bytes) and, transposed, row 4 (l / 16) + (l % 16) / 4
+    static __device__ __forceinline__ uint32_t row_address(uint32_t base, int l)
+    {
+        const int lq = l & 15, g = l >> 4;
+        return base + lq * ROW + ((g ^ swizzle<CPR>(lq)) << 4);
     }
-    store((char *)row_of(p.dQ, b, h, i), dq, scale);
-}
-
-template <int D> __global__ __launch_bounds__(256) void grad_kv_kernel(WindowProblem p, const float *Ds)
-{
-    constexpr int E = D / 64;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)p.batch * p.kv_heads * p.M) return;
-    const int j = (int)(row % p.M), g = (int)(row / p.M % p.kv_heads);
-    const int64_t b = row / p.M / p.kv_heads;
-    const float scale = 1.0f / __builtin_sqrtf((float)D);
-    float q[E], dO[E], k[E], v[E], dk[E] = {}, dv[E] = {};
-    load(k, row_of(p.K, b, g, j));
-    load(v, row_of(p.V, b, g, j));
-    for (int h = g * p.group; h < (g + 1) * p.group; ++h)
-        for (int i = 0; i < p.N; ++i) {
-            if (!sees(i + p.M - p.N, j, p.window, p.sinks)) continue;
-            const int64_t at = (b * p.heads + h) * p.N + i;
-            load(q, row_of(p.Q, b, h, i));
-            load(dO, row_of(p.dO, b, h, i));
-            const float w = expf(dot(q, k) * scale - p.lse[at]), ds = w * (dot(dO, v) - Ds[at]);
+    static __device__ __forceinline__ uint32_t column_address(uint32_t base, int l)
+    {
+        const int lq = l & 15, g = l >> 4, row = 4 * g + (lq >> 2);
+        return base + row * ROW + ((((lq & 3) >> 1) ^ swizzle<CPR>(row)) << 4) + (lq & 1) * 8;
+    }
+    // out[b][n] = tile rows 16 b .. (A operand) times the NB stationary operands x[n][ks], OFF bytes behind `address`
+    template <int OFF, int NB> static __device__ __forceinline__ void products(f32x4 (&out)[2][NB], uint32_t address, const i32x4 (&x)[NB][DS])
+    {
+        constexpr int N = DS * 2;
+        i32x4 f[WIN];
+        static_for<WIN>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            lds_read128<OFF + (i % 2) * 16 * ROW>(f[i], address ^ (i / 2 << 6));
+        });
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                dk[e] = __builtin_fmaf(ds, q[e], dk[e]);
-                dv[e] = __builtin_fmaf(w, dO[e], dv[e]);
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) out[b][n] = (f32x4){0, 0, 0, 0};
+        static_for<N>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value, ks = i / 2, b = i % 2;
+            constexpr int later = N - 1 - i < WIN - 1 ? N - 1 - i : WIN - 1;
+            lds_wait<later>(f[i % WIN]);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) out[b][n] = mfma16(f[i % WIN], x[n][ks], out[b][n]);
+            if constexpr (i + WIN < N) lds_read128<OFF + ((i + WIN) % 2) * 16 * ROW>(f[i % WIN], address ^ ((i + WIN) / 2 << 6));
+        });
+    }
+    // acc[id][n] += (tile)^T y[n]: A operand d 16 id + l % 16, k-slots 0..3 the rows 4 (l / 16) .. +3, k-slots 4..7 those 16 further down
+    template <int OFF, int NB> static __device__ __forceinline__ void accumulate(f32x4 (&acc)[DT][NB], uint32_t address, const i32x4 (&y)[NB])
+    {
+        i32x2 a[WIN], c[WIN];
+        static_for<WIN>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            lds_read_tr64<OFF>(a[i], address ^ (i << 5));
+            lds_read_tr64<OFF + 16 * ROW>(c[i], address ^ (i << 5));
+        });
+        static_for<DT>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            constexpr int later = DT - 1 - i < WIN - 1 ? DT - 1 - i : WIN - 1;
+            lds_wait2<2 * later>(a[i % WIN], c[i % WIN]);
+            const i32x4 f = mfma_frag(a[i % WIN], c[i % WIN]);
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[i][n] = mfma16(f, y[n], acc[i][n]);
+            if constexpr (i + WIN < DT) {
+                lds_read_tr64<OFF>(a[i % WIN], address ^ ((i + WIN) << 5));
+                lds_read_tr64<OFF + 16 * ROW>(c[i % WIN], address ^ ((i + WIN) << 5));
+            }
+        });
+    }
+    // is there an infinity or NaN in the tile?
+    static __device__ __forceinline__ bool any_infinite(const CYC_LDS char *tile, int l)
+    {
+        u16x2 top = {0, 0};
+#pragma unroll 4
+        for (int x = 0; x < TILE * ROW / 1024; ++x) {
+            const i32x4 four = ((const CYC_LDS i32x4 *)tile)[x * 64 + l];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int word = four[r] & 0x7fff7fff;
+                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
             }
         }
-    store((char *)row_of(p.dK, b, g, j), dk, scale);
-    store((char *)row_of(p.dV, b, g, j), dv, 1.0f);
+        const unsigned short t0 = top[0], t1 = top[1];
+        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) >= 0x7f80) != 0;
+    }
+    // accumulate() with the finite values alone; then add(n, value) of every other value, row by row, where seen(row, n)
+    template <int NB, class Seen, class Add>
+    static __device__ __forceinline__ void accumulate_carefully(f32x4 (&acc)[DT][NB], uint32_t address, const CYC_LDS char *tile, int l, const i32x4 (&y)[NB], Seen &&seen, Add &&add)
+    {
+#pragma unroll
+        for (int id = 0; id < DT; ++id) {
+            i32x2 a, c;
+            asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)"
+                         : "=&v"(a), "=&v"(c) : "v"(address ^ (id << 5)), "n"(16 * ROW));
+            const i32x4 clean = {finite_pair(a[0]), finite_pair(a[1]), finite_pair(c[0]), finite_pair(c[1])};
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[id][n] = mfma16(clean, y[n], acc[id][n]);
+        }
+        const int g = l >> 4;
+        for (int r = 0; r < TILE; ++r) {
+            const CYC_LDS char *row = tile + r * ROW;
+            const int word = ((const CYC_LDS int *)row)[l % (ROW / 4)];
+            if (__builtin_amdgcn_ballot_w64(finite_pair(word) != word) == 0) continue;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) {
+                const int chunk = (id * 16 + 4 * g) >> 3, within = ((id * 16 + 4 * g) & 7) * 2;
+                const bf16x4 v = *(const CYC_LDS bf16x4 *)(row + ((chunk ^ swizzle<CPR>(r)) << 4) + within);
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (seen(r, n) && !__builtin_isfinite((float)v[x])) acc[id][n][x] += add((float)v[x]);
+            }
+        }
+    }
+};
+
+// x rounded to bfloat16 as operand of the second products: [key or row block][slot pair], from accumulators [tile half][block]
+template <int NB> __device__ __forceinline__ void pack(i32x4 (&y)[NB], const f32x4 (&x)[2][NB])
+{
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int r = 0; r < 4; r += 2) {
+                const bf16x2 pair = __builtin_convertvector((f32x2){x[b][n][r], x[b][n][r + 1]}, bf16x2);
+                y[n][b * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
+            }
+}
+
+__device__ __forceinline__ float not_a_number(float) { return __builtin_nanf(""); }
+__device__ __forceinline__ float itself(float x) { return x; }
+
+// lse and D of every row by head, lse in the log2 domain, heads padded to whole tiles
+__host__ __device__ inline int64_t padded_rows(int N) { return ((int64_t)N + TILE - 1) / TILE * TILE; }
+
+// ---- dQ.  A workgroup of four waves keeps 128 rows r (query r / group, head r % group of a key head) and walks the keys that any of them
+// sees in tiles of 64, two steps of 32 to a barrier.  Also writes lse and D of its rows for the other kernel.
+constexpr int KEY_TILE = 64;
+
+template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const WindowProblem p, int tiles, float scale, float *lse2, float *Ds)
+{
+    typedef Tile<D> T;
+    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, QB = 2, QW = 32, ROWS = 128;
+    constexpr int TILE_BYTES = KEY_TILE * ROW, COPIES = TILE_BYTES / 4096, RPC = 64 / CPR;
+    __shared__ __attribute__((aligned(1024))) char lds_raw[4 * TILE_BYTES];        // two stages of K, then two of V
+    CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int total = gridDim.x, xcd = blockIdx.x & 7;                              // (see tile_kernel)
+    const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+    const int tile = tiles - 1 - at % tiles, head = at / tiles % p.kv_heads;
+    const int64_t b = at / tiles / p.kv_heads;
+    const int group = p.group, N = p.N, M = p.M, R = N * group, window = p.window, sinks = p.sinks;
+    const char *K = p.K.base + b * p.K.batch + head * p.K.head, *V = p.V.base + b * p.V.batch + head * p.V.head;
+    const int64_t k_row = p.K.row, v_row = p.V.row;
+
+    const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
+    const int p_first = row_first / group + M - N, hi = row_last / group + M - N;
+    const int lo = p_first >= window ? p_first - window + 1 : 0;
+    const int sink_end = sinks < lo ? sinks : lo;
+    const int sink_tiles = (sink_end + KEY_TILE - 1) / KEY_TILE, window_tile = lo / KEY_TILE > sink_tiles ? lo / KEY_TILE : sink_tiles;
+    const int ntiles = hi < 0 ? 0 : sink_tiles + (hi / KEY_TILE - window_tile + 1 > 0 ? hi / KEY_TILE - window_tile + 1 : 0);
+    auto tile_key = [&](int u) __attribute__((always_inline)) { return (u < sink_tiles ? u : window_tile - sink_tiles + u) * KEY_TILE; };
+    auto seen_key = [&](int key) __attribute__((always_inline)) {
+        key = key < hi ? key : hi;
+        return key >= sink_end && key < lo ? lo : key;
+    };
+
+    const int r0 = row_first + w * QW;
+    const bool idle = r0 > row_last;
+    const int p_lo = idle ? 0 : __builtin_amdgcn_readfirstlane(r0 / group + M - N);
+    const int r_last = r0 + QW - 1 < row_last ? r0 + QW - 1 : row_last;
+    const int p_hi = idle ? -1 : __builtin_amdgcn_readfirstlane(r_last / group + M - N);
+    int row_hi[QB], row_lo[QB];
+    float lse[QB], Di[QB];
+    i32x4 qf[QB][DS], of[QB][DS];
+#pragma unroll
+    for (int jq = 0; jq < QB; ++jq) {
+        int r = r0 + jq * 16 + lq;
+        const bool mine = r <= row_last;
+        r = mine ? r : row_last;
+        const int i = r / group, h = head * group + r - i * group;
+        row_hi[jq] = i + M - N;
+        row_lo[jq] = (row_hi[jq] < 0 ? 0 : row_hi[jq]) - window + 1;
+        const char *q = p.Q.base + b * p.Q.batch + h * p.Q.head + i * p.Q.row + g * 16, *o = p.O.base + b * p.O.batch + h * p.O.head + i * p.O.row + g * 16;
+        const char *dO = p.dO.base + b * p.dO.batch + h * p.dO.head + i * p.dO.row + g * 16;
+        float dot = 0;
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+            qf[jq][ks] = *(const i32x4 *)(q + ks * 64);
+            of[jq][ks] = *(const i32x4 *)(dO + ks * 64);
+            const bf16x8 x = *(const bf16x8 *)(o + ks * 64), y = __builtin_bit_cast(bf16x8, of[jq][ks]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dot = __builtin_fmaf((float)x[e], (float)y[e], dot);
+        }
+        Di[jq] = query_sum(dot);
+        const int64_t row = b * p.heads + h;
+        lse[jq] = p.lse[row * N + i] * 1.4426950408889634f;
+        if (mine && g == 0) {
+            lse2[row * padded_rows(N) + i] = lse[jq];
+            Ds[row * padded_rows(N) + i] = Di[jq];
+        }
+    }
+
+    const int row0 = w * RPC + l / CPR;
+    auto issue = [&](int u) __attribute__((always_inline)) {
+        const int k0 = tile_key(u);
+        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES + w * 1024;
+#pragma unroll
+        for (int x = 0; x < COPIES; ++x) {
+            const int r = x * (4 * RPC) + row0, key = seen_key(k0 + r), chunk = ((l % CPR) ^ swizzle<CPR>(r)) << 4;
+            copy16_from(K + key * k_row + chunk, dst + x * 4096);
+            copy16_from(V + key * v_row + chunk, dst + 2 * TILE_BYTES + x * 4096);
+        }
+    };
+
+    f32x4 acc[DT][QB];
+#pragma unroll
+    for (int id = 0; id < DT; ++id)
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq) acc[id][jq] = (f32x4){0, 0, 0, 0};
+    uint32_t by_row = T::row_address(lds_base, l), by_column = T::column_address(lds_base, l);
+    if (ntiles > 0) issue(0);
+    for (int u = 0; u < ntiles; ++u) {
+        landed_barrier();
+        if (u + 1 < ntiles) issue(u + 1);
+#pragma unroll 1
+        for (int half = 0; half < KEY_TILE / TILE; ++half) {
+            const int k0 = tile_key(u) + half * TILE, k1 = k0 + TILE - 1;
+            const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
+            if (!none) {
+                const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
+                f32x4 s[2][QB], dp[2][QB];                       // S^T and dP^T: [16 keys][16 rows]
+                T::template products<0>(s, by_row, qf);
+                T::template products<2 * TILE_BYTES>(dp, by_row, of);
+                auto visible = [&](int key, int jq) __attribute__((always_inline)) { return key <= row_hi[jq] && (key >= row_lo[jq] || key < sinks); };
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][jq][r], scale, -lse[jq]));
+                            s[c][jq][r] = P * (dp[c][jq][r] - Di[jq]);
+                        }
+                bool careful = false;
+                const CYC_LDS char *here = lds + (u & 1) * TILE_BYTES + half * TILE * ROW;
+                if (!all) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) s[c][jq][r] = visible(k0 + c * 16 + 4 * g + r, jq) ? s[c][jq][r] : 0.0f;
+                    careful = T::any_infinite(here, l);
+                }
+                i32x4 y[QB];
+                pack(y, s);
+                if (__builtin_expect(careful, 0)) T::accumulate_carefully(acc, by_column, here, l, y, [&](int r, int jq) { return visible(k0 + r, jq); }, not_a_number);
+                else T::template accumulate<0>(acc, by_column, y);
+            }
+            by_row += TILE * ROW;
+            by_column += TILE * ROW;
+        }
+        const int turn = u & 1 ? -2 * TILE_BYTES : 0;                                // both halves done: the other stage follows, or the first
+        by_row += turn;
+        by_column += turn;
+    }
+
+    const float back = 1.0f / __builtin_sqrtf((float)D);
+#pragma unroll
+    for (int jq = 0; jq < QB; ++jq) {
+        const int r = r0 + jq * 16 + lq;
+        if (r > row_last) continue;
+        const int i = r / group, h = head * group + r - i * group;
+        char *dq = (char *)p.dQ.base + b * p.dQ.batch + h * p.dQ.head + i * p.dQ.row;
+#pragma unroll
+        for (int id = 0; id < DT; ++id) {
+            bf16x4 o;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] = (__bf16)(acc[id][jq][x] * back);
+            *(bf16x4 *)(dq + (id * 16 + 4 * g) * 2) = o;
+        }
+    }
+}
+
+// ---- dK and dV.  A workgroup of four waves keeps 64 * KB keys of one key head and walks the rows that see any of them, head after head in
+// tiles of 32 queries.  Keys that many rows see, the sinks before all, and keys of calls with few of them have their rows cut into runs,
+// which different workgroups take and a second kernel adds up in ascending order.
+struct Runs {
+    int tiles;                           // tiles of keys
+    int first, first_runs, runs;         // tiles below `first` have first_runs runs, the others `runs`
+    __host__ __device__ int per_pair() const { return first * first_runs + (tiles - first) * runs; }
+    // partial sums kept: those of the first tiles, and of the others where they have more than one run
+    __host__ __device__ int kept_tiles() const { return runs > 1 ? tiles : first_runs > 1 ? first : 0; }
+    __host__ __device__ int kept_per_pair() const { return runs > 1 ? per_pair() : first_runs > 1 ? first * first_runs : 0; }
+    __host__ __device__ int slot(int tile) const { return tile < first ? tile * first_runs : first * first_runs + (tile - first) * runs; }
+    __host__ __device__ int runs_of(int tile) const { return tile < first ? first_runs : runs; }
+};
+
+template <int D> constexpr int KEY_BLOCKS = 256 / D;      // 16-key blocks of a wave: what the registers hold
+template <int D> constexpr int KEYS = 64 * KEY_BLOCKS<D>;
+
+template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part)
+{
+    typedef Tile<D> T;
+    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS<D>, KW = 16 * KB;
+    constexpr int TILE_BYTES = TILE * ROW, COPIES = TILE_BYTES / 1024, RPC = 64 / CPR, STAGE = 2 * TILE_BYTES + 1024;
+    // a stage: the tile of Q, that of dO, lse and D of its rows
+    __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE];
+    CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
+    const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
+    const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int total = gridDim.x, xcd = blockIdx.x & 7;
+    const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+    const int per_pair = runs.per_pair(), pair = at / per_pair, slot = at - pair * per_pair;
+    const int in_first = runs.first * runs.first_runs;
+    const int tile = slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs;
+    const int run = slot - runs.slot(tile), nruns = runs.runs_of(tile);
+    const int head = pair % p.kv_heads;
+    const int64_t b = pair / p.kv_heads;
+    const int group = p.group, N = p.N, M = p.M, window = p.window, sinks = p.sinks;
+
+    // ---- the queries that see any of the keys k_first .. k_last, and this run's share of the tiles (head, 32 queries)
+    const int k_first = tile * KEYS<D>, k_last = (M - k_first < KEYS<D> ? M : k_first + KEYS<D>) - 1;
+    const int i_first = k_first - (M - N) > 0 ? k_first - (M - N) : 0;
+    const int64_t reach = (int64_t)k_last + window - 1 - (M - N);
+    const int i_last = k_first < sinks || reach > N - 1 ? N - 1 : (int)reach;
+    const int t_first = i_first / TILE, per_head = i_last >= i_first ? i_last / TILE - t_first + 1 : 0;
+    const int all_tiles = per_head * group;
+    const int u_first = (int)((int64_t)all_tiles * run / nruns), u_last = (int)((int64_t)all_tiles * (run + 1) / nruns);
+
+    // ---- this wave's keys as B operands
+    const int kw = k_first + w * KW, kw_last = kw + KW - 1;
+    i32x4 kf[KB][DS], vf[KB][DS];
+#pragma unroll
+    for (int n = 0; n < KB; ++n) {
+        int key = kw + n * 16 + lq;
+        key = key < M ? key : M - 1;
+        const char *k = p.K.base + b * p.K.batch + head * p.K.head + key * p.K.row + g * 16, *v = p.V.base + b * p.V.batch + head * p.V.head + key * p.V.row + g * 16;
+#pragma unroll
+        for (int ks = 0; ks < DS; ++ks) {
+            kf[n][ks] = *(const i32x4 *)(k + ks * 64);
+            vf[n][ks] = *(const i32x4 *)(v + ks * 64);
+        }
+    }
+
+    const int64_t q_row = p.Q.row, q_head = p.Q.head, o_row = p.dO.row, o_head = p.dO.head, padded = padded_rows(N);
+    const char *Q = p.Q.base + b * p.Q.batch + head * group * q_head, *dO = p.dO.base + b * p.dO.batch + head * group * o_head;
+    const float *stats = (l < 32 ? lse2 : Ds) + (b * p.heads + head * group) * padded + (l & 31);
+    auto issue = [&](int u) __attribute__((always_inline)) {
+        const int h = u / per_head, i0 = (t_first + u - h * per_head) * TILE;        // uniform
+        const uint32_t dst = lds_base + ((u - u_first) & 1) * STAGE;
+#pragma unroll
+        for (int x = 0; x < COPIES; x += 4) {
+            // copies x .. x+3 are shared out among the four waves, one each
+            const int r = (x + w) * RPC + l / CPR, i = i0 + r < N ? i0 + r : N - 1, chunk = ((l % CPR) ^ swizzle<CPR>(r)) << 4;
+            copy16_from(Q + h * q_head + i * q_row + chunk, dst + (x + w) * 1024);
+            copy16_from(dO + h * o_head + i * o_row + chunk, dst + TILE_BYTES + (x + w) * 1024);
+        }
+        if (w == 0)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(dst + 2 * TILE_BYTES), "v"(stats + h * padded + i0) : "memory", "m0");
+    };
+
+    f32x4 dk[DT][KB], dv[DT][KB];
+#pragma unroll
+    for (int id = 0; id < DT; ++id)
+#pragma unroll
+        for (int n = 0; n < KB; ++n) dk[id][n] = dv[id][n] = (f32x4){0, 0, 0, 0};
+    uint32_t by_row = T::row_address(lds_base, l), by_column = T::column_address(lds_base, l);
+    if (u_first < u_last) issue(u_first);
+    for (int u = u_first; u < u_last; ++u) {
+        landed_barrier();
+        if (u + 1 < u_last) issue(u + 1);
+        const int stage = (u - u_first) & 1, i0 = (t_first + u % per_head) * TILE;
+        const int p0 = i0 + M - N, p1 = (i0 + TILE < N ? i0 + TILE : N) - 1 + M - N;
+        const bool none = kw >= M || p1 < kw || (kw >= sinks && (int64_t)p0 - kw_last >= window);
+        if (!none) {
+            const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
+            const CYC_LDS char *here = lds + stage * STAGE;
+            uint32_t row_address = by_row, column_address = by_column;
+            asm("" : "+v"(row_address), "+v"(column_address));       // (the addresses that derive from them are cheaper taken than kept)
+            f32x4 s[2][KB], dp[2][KB];                               // S and dP: [16 queries][16 keys]
+            T::template products<0>(s, row_address, kf);
+            T::template products<TILE_BYTES>(dp, row_address, vf);
+            auto visible = [&](int r, int n) __attribute__((always_inline)) {
+                const int position = p0 + r, key = kw + n * 16 + lq;
+                return i0 + r < N && key <= position && (position - key < window || key < sinks);
+            };
+            i32x4 py[KB];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const f32x4 lse = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + (c * 16 + 4 * g) * 4);
+                const f32x4 Di = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + 128 + (c * 16 + 4 * g) * 4);
+#pragma unroll
+                for (int n = 0; n < KB; ++n)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], scale, -lse[r]));
+                        s[c][n][r] = P;
+                        dp[c][n][r] = P * (dp[c][n][r] - Di[r]);
+                    }
+            }
+            bool careful_q = false, careful_o = false;
+            if (!all) {
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int n = 0; n < KB; ++n)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const bool seen = visible(c * 16 + 4 * g + r, n);
+                            s[c][n][r] = seen ? s[c][n][r] : 0.0f;
+                            dp[c][n][r] = seen ? dp[c][n][r] : 0.0f;
+                        }
+                careful_q = T::any_infinite(here, l);
+                careful_o = T::any_infinite(here + TILE_BYTES, l);
+            }
+            pack(py, s);
+            if (__builtin_expect(careful_o, 0)) T::accumulate_carefully(dv, column_address + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
+            else T::template accumulate<TILE_BYTES>(dv, column_address, py);
+            pack(py, dp);
+            if (__builtin_expect(careful_q, 0)) T::accumulate_carefully(dk, column_address, here, l, py, visible, not_a_number);
+            else T::template accumulate<0>(dk, column_address, py);
+        }
+        const int turn = stage ? -STAGE : STAGE;
+        by_row += turn;
+        by_column += turn;
+    }
+
+    // accumulator register r of lane l: d = 16 id + 4 (l/16) + r, key kw + 16 n + l%16
+    const float back = 1.0f / __builtin_sqrtf((float)D);
+#pragma unroll
+    for (int n = 0; n < KB; ++n) {
+        const int key = kw + n * 16 + lq;
+        if (nruns > 1) {
+            float *to = part + (((int64_t)pair * runs.kept_per_pair() + slot) * 2 * KEYS<D> + w * KW + n * 16 + lq) * D;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) {
+                *(f32x4 *)(to + id * 16 + 4 * g) = dk[id][n];
+                *(f32x4 *)(to + (int64_t)KEYS<D> * D + id * 16 + 4 * g) = dv[id][n];
+            }
+            continue;
+        }
+        if (key >= M) continue;
+        char *to_k = (char *)p.dK.base + b * p.dK.batch + head * p.dK.head + key * p.dK.row, *to_v = (char *)p.dV.base + b * p.dV.batch + head * p.dV.head + key * p.dV.row;
+#pragma unroll
+        for (int id = 0; id < DT; ++id) {
+            bf16x4 x, y;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x[r] = (__bf16)(dk[id][n][r] * back);
+                y[r] = (__bf16)dv[id][n][r];
+            }
+            *(bf16x4 *)(to_k + (id * 16 + 4 * g) * 2) = x;
+            *(bf16x4 *)(to_v + (id * 16 + 4 * g) * 2) = y;
+        }
+    }
+}
+
+// Adds the runs of a tile of keys in ascending order; a thread takes four d of a key's dK and dV.
+template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part)
+{
+    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int c = (int)(x % (D / 4)) * 4, in_tile = (int)(x / (D / 4) % KEYS<D>);
+    const int64_t rest = x / (D / 4) / KEYS<D>;
+    const int tile = (int)(rest % runs.kept_tiles());
+    const int64_t pair = rest / runs.kept_tiles(), b = pair / p.kv_heads;
+    const int head = (int)(pair % p.kv_heads), key = tile * KEYS<D> + in_tile;
+    if (b >= p.batch || key >= p.M || runs.runs_of(tile) <= 1) return;
+    const float *from = part + ((pair * runs.kept_per_pair() + runs.slot(tile)) * 2 * KEYS<D> + in_tile) * D + c;
+    f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
+    for (int run = 0; run < runs.runs_of(tile); ++run, from += 2 * KEYS<D> * D) {
+        dk += *(const f32x4 *)from;
+        dv += *(const f32x4 *)(from + KEYS<D> * D);
+    }
+    const float back = 1.0f / __builtin_sqrtf((float)D);
+    bf16x4 u, v;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        u[r] = (__bf16)(dk[r] * back);
+        v[r] = (__bf16)dv[r];
+    }
+    *(bf16x4 *)((char *)p.dK.base + b * p.dK.batch + head * p.dK.head + key * p.dK.row + c * 2) = u;
+    *(bf16x4 *)((char *)p.dV.base + b * p.dV.batch + head * p.dV.head + key * p.dV.row + c * 2) = v;
+}
+
+// The chip takes 512 workgroups at a time.  With fewer tiles of keys than that their rows are cut into runs of at least eight steps; the
+// tiles of sinks, which every later row sees, into runs as long as the other tiles' work.
+Runs choose_runs(const WindowProblem &p)
+{
+    const int keys = p.d == 128 ? KEYS<128> : KEYS<64>;
+    Runs r = {(p.M + keys - 1) / keys, 0, 1, 1};
+    const int64_t pairs = (int64_t)p.batch * p.kv_heads;
+    const int64_t usual = std::min<int64_t>(p.N, (int64_t)p.window + keys), steps = (usual + TILE - 1) / TILE * p.group;
+    const int64_t all_steps = ((int64_t)p.N + TILE - 1) / TILE * p.group;
+    r.runs = (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(1, pairs * r.tiles), steps / 8, (int64_t)64}));
+    r.first = (int)std::min<int64_t>(r.tiles, ((int64_t)std::min(p.sinks, p.M) + keys - 1) / keys);
+    if (p.window == INT_MAX) r.first = 0;
+    const int64_t run_steps = std::max<int64_t>(1, (steps + r.runs - 1) / r.runs);
+    r.first_runs = (int)std::max<int64_t>(r.runs, std::min<int64_t>((all_steps + run_steps - 1) / run_steps, 256));
+    if (r.first == 0) r.first_runs = r.runs;
+    return r;
+}
+
+int64_t stats_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * padded_rows(p.N) * 8 + 255) / 256 * 256; }
+
+template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace, hipStream_t s)
+{
+    float *lse2 = (float *)workspace, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)((char *)workspace + stats_bytes(p));
+    const float scale = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
+    const int tiles = (int)(((int64_t)p.N * p.group + 127) / 128);
+    const int64_t pairs = (int64_t)p.batch * p.kv_heads;
+    const Runs runs = choose_runs(p);
+    if (tiles * pairs >= ((int64_t)1 << 31) || runs.per_pair() * pairs >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+    hipError_t e = hipSuccess;
+    if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs)), dim3(256), s, p, tiles, scale, lse2, Ds);
+    if (e != hipSuccess || p.M == 0) return e;
+    e = launch_kernel(grad_kv_kernel<D>, dim3((unsigned)(runs.per_pair() * pairs)), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part);
+    if (e != hipSuccess || runs.kept_tiles() == 0) return e;
+    const int64_t threads = pairs * runs.kept_tiles() * KEYS<D> * (D / 4);
+    return launch_kernel(grad_join_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), s, p, runs, (const float *)part);
 }
 
 }  // namespace
 
-int64_t window_grad_workspace_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * p.N * 4 + 15) / 16 * 16; }
+int64_t window_grad_workspace_bytes(const WindowProblem &p)
+{
+    const int64_t keys = p.d == 128 ? KEYS<128> : KEYS<64>;
+    return stats_bytes(p) + (p.M > 0 ? (int64_t)p.batch * p.kv_heads * choose_runs(p).kept_per_pair() * 2 * keys * p.d * 4 : 0);
+}
 
 hipError_t launch_window_grad(const WindowProblem &p, void *workspace, int64_t, hipStream_t s)
 {
-    const int64_t rows = (int64_t)p.batch * p.heads * p.N, keys = (int64_t)p.batch * p.kv_heads * p.M;
-    const dim3 grid((unsigned)((rows + 3) / 4)), kgrid((unsigned)((keys + 3) / 4)), block(256);
-    float *Ds = (float *)workspace;
-    hipError_t e = hipSuccess;
-    if (rows) e = p.d == 128 ? launch_kernel(grad_q_kernel<128>, grid, block, s, p, Ds) : launch_kernel(grad_q_kernel<64>, grid, block, s, p, Ds);
-    if (e != hipSuccess || keys == 0) return e;
-    return p.d == 128 ? launch_kernel(grad_kv_kernel<128>, kgrid, block, s, p, (const float *)Ds)
-                      : launch_kernel(grad_kv_kernel<64>, kgrid, block, s, p, (const float *)Ds);
+    return p.d == 128 ? launch_grad<128>(p, workspace, s) : launch_grad<64>(p, workspace, s);
 }
 
 }  // namespace cyc
