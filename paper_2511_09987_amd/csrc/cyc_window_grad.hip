@@ -21,9 +21,14 @@
 namespace cyc {
 namespace {
 
-// In a tile of rows of ROW bytes chunk c of row r sits in slot c ^ swizzle(r): the 16 rows that a row-wise read touches fall on
-// distinct banks, and so do the eight rows of half a transposing read.  Linear in the bits of r.
-template <int CPR> __device__ __forceinline__ constexpr int swizzle(int r) { return CPR == 16 ? ((r & 7) << 1 | (r >> 3 & 1)) : ((r >> 1 & 3) << 1 | (r >> 3 & 1)); }
+// In a tile of rows of ROW bytes chunk c of row r sits in slot c ^ swizzle(r).  Sixteen lanes read 16 bytes each of a row-wise operand at
+// a time, rows 0-3 and 12-15 at one chunk and 4-11 at its neighbour (or the other way round), and eight rows of 32 bytes of a transposed
+// one: with this map both fall on all 64 banks.  Linear in the bits of r.
+template <int CPR> __device__ __forceinline__ constexpr int swizzle(int r)
+{
+    const int high = r >> 3 & 1;
+    return CPR == 16 ? ((r & 7) ^ high << 2) << 1 | high : ((r >> 1 & 3) ^ high << 1) << 1 | high;
+}
 
 constexpr int TILE = 32;                 // rows of a tile of queries, keys of a step
 
@@ -41,26 +46,29 @@ template <int D> struct Tile {
         const int lq = l & 15, g = l >> 4, row = 4 * g + (lq >> 2);
         return base + row * ROW + ((((lq & 3) >> 1) ^ swizzle<CPR>(row)) << 4) + (lq & 1) * 8;
     }
-    // out[b][n] = tile rows 16 b .. (A operand) times the NB stationary operands x[n][ks], OFF bytes behind `address`
-    template <int OFF, int NB> static __device__ __forceinline__ void products(f32x4 (&out)[2][NB], uint32_t address, const i32x4 (&x)[NB][DS])
+    // first[n] and second[n] = rows 16 H .. 16 H + 15 of the tile (A operand) that lies A bytes, resp. B bytes, behind `address`, times the NB
+    // stationary operands x[n][ks], resp. y[n][ks]
+    template <int H, int A, int B, int NB>
+    static __device__ __forceinline__ void products(f32x4 (&first)[NB], f32x4 (&second)[NB], uint32_t address, const i32x4 (&x)[NB][DS], const i32x4 (&y)[NB][DS])
     {
         constexpr int N = DS * 2;
         i32x4 f[WIN];
         static_for<WIN>([&](auto ic) __attribute__((always_inline)) {
             constexpr int i = decltype(ic)::value;
-            lds_read128<OFF + (i % 2) * 16 * ROW>(f[i], address ^ (i / 2 << 6));
+            lds_read128<(i < DS ? A : B) + H * 16 * ROW>(f[i], address ^ (i % DS << 6));
         });
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int n = 0; n < NB; ++n) out[b][n] = (f32x4){0, 0, 0, 0};
+        for (int n = 0; n < NB; ++n) first[n] = second[n] = (f32x4){0, 0, 0, 0};
         static_for<N>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, ks = i / 2, b = i % 2;
+            constexpr int i = decltype(ic)::value, ks = i % DS, next = i + WIN;
             constexpr int later = N - 1 - i < WIN - 1 ? N - 1 - i : WIN - 1;
             lds_wait<later>(f[i % WIN]);
 #pragma unroll
-            for (int n = 0; n < NB; ++n) out[b][n] = mfma16(f[i % WIN], x[n][ks], out[b][n]);
-            if constexpr (i + WIN < N) lds_read128<OFF + ((i + WIN) % 2) * 16 * ROW>(f[i % WIN], address ^ ((i + WIN) / 2 << 6));
+            for (int n = 0; n < NB; ++n) {
+                if constexpr (i < DS) first[n] = mfma16(f[i % WIN], x[n][ks], first[n]);
+                else second[n] = mfma16(f[i % WIN], y[n][ks], second[n]);
+            }
+            if constexpr (next < N) lds_read128<(next < DS ? A : B) + H * 16 * ROW>(f[i % WIN], address ^ (next % DS << 6));
         });
     }
     // acc[id][n] += (tile)^T y[n]: A operand d 16 id + l % 16, k-slots 0..3 the rows 4 (l / 16) .. +3, k-slots 4..7 those 16 further down
@@ -133,18 +141,16 @@ template <int D> struct Tile {
     }
 };
 
-// x rounded to bfloat16 as operand of the second products: [key or row block][slot pair], from accumulators [tile half][block]
-template <int NB> __device__ __forceinline__ void pack(i32x4 (&y)[NB], const f32x4 (&x)[2][NB])
+// x rounded to bfloat16 as half H of an operand of the second products
+template <int H, int NB> __device__ __forceinline__ void pack(i32x4 (&y)[NB], const f32x4 (&x)[NB])
 {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int r = 0; r < 4; r += 2) {
-                const bf16x2 pair = __builtin_convertvector((f32x2){x[b][n][r], x[b][n][r + 1]}, bf16x2);
-                y[n][b * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
-            }
+        for (int r = 0; r < 4; r += 2) {
+            const bf16x2 pair = __builtin_convertvector((f32x2){x[n][r], x[n][r + 1]}, bf16x2);
+            y[n][H * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
+        }
 }
 
 __device__ __forceinline__ float not_a_number(float) { return __builtin_nanf(""); }
@@ -250,32 +256,29 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
             const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
             if (!none) {
                 const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
-                f32x4 s[2][QB], dp[2][QB];                       // S^T and dP^T: [16 keys][16 rows]
-                T::template products<0>(s, by_row, qf);
-                T::template products<2 * TILE_BYTES>(dp, by_row, of);
                 auto visible = [&](int key, int jq) __attribute__((always_inline)) { return key <= row_hi[jq] && (key >= row_lo[jq] || key < sinks); };
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
+                i32x4 y[QB];                                     // dS^T as B operand
+                static_for<2>([&](auto cc) __attribute__((always_inline)) {
+                    constexpr int c = decltype(cc)::value;
+                    f32x4 s[QB], dp[QB];                         // S^T and dP^T: 16 keys x [16 rows]
+                    T::template products<c, 0, 2 * TILE_BYTES>(s, dp, by_row, qf, of);
 #pragma unroll
                     for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
-                            const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][jq][r], scale, -lse[jq]));
-                            s[c][jq][r] = P * (dp[c][jq][r] - Di[jq]);
+                            const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[jq][r], scale, -lse[jq]));
+                            s[jq][r] = P * (dp[jq][r] - Di[jq]);
                         }
-                bool careful = false;
-                const CYC_LDS char *here = lds + (u & 1) * TILE_BYTES + half * TILE * ROW;
-                if (!all) {
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                    if (!all) {
 #pragma unroll
                         for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) s[c][jq][r] = visible(k0 + c * 16 + 4 * g + r, jq) ? s[c][jq][r] : 0.0f;
-                    careful = T::any_infinite(here, l);
-                }
-                i32x4 y[QB];
-                pack(y, s);
+                            for (int r = 0; r < 4; ++r) s[jq][r] = visible(k0 + c * 16 + 4 * g + r, jq) ? s[jq][r] : 0.0f;
+                    }
+                    pack<c>(y, s);
+                });
+                const CYC_LDS char *here = lds + (u & 1) * TILE_BYTES + half * TILE * ROW;
+                const bool careful = !all && T::any_infinite(here, l);
                 if (__builtin_expect(careful, 0)) T::accumulate_carefully(acc, by_column, here, l, y, [&](int r, int jq) { return visible(k0 + r, jq); }, not_a_number);
                 else T::template accumulate<0>(acc, by_column, y);
             }
@@ -318,13 +321,17 @@ struct Runs {
     __host__ __device__ int runs_of(int tile) const { return tile < first ? first_runs : runs; }
 };
 
-template <int D> constexpr int KEY_BLOCKS = 256 / D;      // 16-key blocks of a wave: what the registers hold
-template <int D> constexpr int KEYS = 64 * KEY_BLOCKS<D>;
+constexpr int KEY_BLOCKS = 2;            // 16-key blocks of a wave: what the registers hold at d = 128
+constexpr int KEYS = 64 * KEY_BLOCKS;
 
-template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part)
+// The code for tiles that are not all finite takes registers that the usual case does not have to spare (96 of them spilled, and
+// half the speed), so it has a launch of its own: CAREFUL false does without and leaves a mark where it met such a masked tile, CAREFUL true
+// does the marked workgroups again.
+template <int D, bool CAREFUL>
+__global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
 {
     typedef Tile<D> T;
-    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS<D>, KW = 16 * KB;
+    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB;
     constexpr int TILE_BYTES = TILE * ROW, COPIES = TILE_BYTES / 1024, RPC = 64 / CPR, STAGE = 2 * TILE_BYTES + 1024;
     // a stage: the tile of Q, that of dO, lse and D of its rows
     __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE];
@@ -333,6 +340,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const 
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int total = gridDim.x, xcd = blockIdx.x & 7;
     const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
+    if (CAREFUL && marks[at * 4] + marks[at * 4 + 1] + marks[at * 4 + 2] + marks[at * 4 + 3] == 0) return;
+    bool marked = false;
     const int per_pair = runs.per_pair(), pair = at / per_pair, slot = at - pair * per_pair;
     const int in_first = runs.first * runs.first_runs;
     const int tile = slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs;
@@ -342,7 +351,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const 
     const int group = p.group, N = p.N, M = p.M, window = p.window, sinks = p.sinks;
 
     // ---- the queries that see any of the keys k_first .. k_last, and this run's share of the tiles (head, 32 queries)
-    const int k_first = tile * KEYS<D>, k_last = (M - k_first < KEYS<D> ? M : k_first + KEYS<D>) - 1;
+    const int k_first = tile * KEYS, k_last = (M - k_first < KEYS ? M : k_first + KEYS) - 1;
     const int i_first = k_first - (M - N) > 0 ? k_first - (M - N) : 0;
     const int64_t reach = (int64_t)k_last + window - 1 - (M - N);
     const int i_last = k_first < sinks || reach > N - 1 ? N - 1 : (int)reach;
@@ -400,65 +409,65 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const 
             const CYC_LDS char *here = lds + stage * STAGE;
             uint32_t row_address = by_row, column_address = by_column;
             asm("" : "+v"(row_address), "+v"(column_address));       // (the addresses that derive from them are cheaper taken than kept)
-            f32x4 s[2][KB], dp[2][KB];                               // S and dP: [16 queries][16 keys]
-            T::template products<0>(s, row_address, kf);
-            T::template products<TILE_BYTES>(dp, row_address, vf);
             auto visible = [&](int r, int n) __attribute__((always_inline)) {
                 const int position = p0 + r, key = kw + n * 16 + lq;
                 return i0 + r < N && key <= position && (position - key < window || key < sinks);
             };
-            i32x4 py[KB];
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            i32x4 py[KB], dsy[KB];                                   // P and dS as B operands
+            static_for<2>([&](auto cc) __attribute__((always_inline)) {
+                constexpr int c = decltype(cc)::value;
+                f32x4 s[KB], dp[KB];                                 // S and dP: 16 queries x [16 keys]
+                T::template products<c, 0, TILE_BYTES>(s, dp, row_address, kf, vf);
                 const f32x4 lse = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + (c * 16 + 4 * g) * 4);
                 const f32x4 Di = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + 128 + (c * 16 + 4 * g) * 4);
 #pragma unroll
                 for (int n = 0; n < KB; ++n)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], scale, -lse[r]));
-                        s[c][n][r] = P;
-                        dp[c][n][r] = P * (dp[c][n][r] - Di[r]);
+                        const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], scale, -lse[r]));
+                        s[n][r] = P;
+                        dp[n][r] = P * (dp[n][r] - Di[r]);
                     }
-            }
-            bool careful_q = false, careful_o = false;
-            if (!all) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c)
+                if (!all) {
 #pragma unroll
                     for (int n = 0; n < KB; ++n)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             const bool seen = visible(c * 16 + 4 * g + r, n);
-                            s[c][n][r] = seen ? s[c][n][r] : 0.0f;
-                            dp[c][n][r] = seen ? dp[c][n][r] : 0.0f;
+                            s[n][r] = seen ? s[n][r] : 0.0f;
+                            dp[n][r] = seen ? dp[n][r] : 0.0f;
                         }
-                careful_q = T::any_infinite(here, l);
-                careful_o = T::any_infinite(here + TILE_BYTES, l);
+                }
+                pack<c>(py, s);
+                pack<c>(dsy, dp);
+            });
+            const bool careful = !all && (T::any_infinite(here, l) || T::any_infinite(here + TILE_BYTES, l));
+            if (CAREFUL && careful) {
+                T::accumulate_carefully(dv, column_address + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
+                T::accumulate_carefully(dk, column_address, here, l, dsy, visible, not_a_number);
+            } else {
+                marked |= careful;
+                T::template accumulate<TILE_BYTES>(dv, column_address, py);
+                T::template accumulate<0>(dk, column_address, dsy);
             }
-            pack(py, s);
-            if (__builtin_expect(careful_o, 0)) T::accumulate_carefully(dv, column_address + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
-            else T::template accumulate<TILE_BYTES>(dv, column_address, py);
-            pack(py, dp);
-            if (__builtin_expect(careful_q, 0)) T::accumulate_carefully(dk, column_address, here, l, py, visible, not_a_number);
-            else T::template accumulate<0>(dk, column_address, py);
         }
         const int turn = stage ? -STAGE : STAGE;
         by_row += turn;
         by_column += turn;
     }
 
+    if (!CAREFUL && l == 0) marks[at * 4 + w] = marked;
     // accumulator register r of lane l: d = 16 id + 4 (l/16) + r, key kw + 16 n + l%16
     const float back = 1.0f / __builtin_sqrtf((float)D);
 #pragma unroll
     for (int n = 0; n < KB; ++n) {
         const int key = kw + n * 16 + lq;
         if (nruns > 1) {
-            float *to = part + (((int64_t)pair * runs.kept_per_pair() + slot) * 2 * KEYS<D> + w * KW + n * 16 + lq) * D;
+            float *to = part + (((int64_t)pair * runs.kept_per_pair() + slot) * 2 * KEYS + w * KW + n * 16 + lq) * D;
 #pragma unroll
             for (int id = 0; id < DT; ++id) {
                 *(f32x4 *)(to + id * 16 + 4 * g) = dk[id][n];
-                *(f32x4 *)(to + (int64_t)KEYS<D> * D + id * 16 + 4 * g) = dv[id][n];
+                *(f32x4 *)(to + (int64_t)KEYS * D + id * 16 + 4 * g) = dv[id][n];
             }
             continue;
         }
@@ -482,17 +491,17 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const 
 template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part)
 {
     const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int c = (int)(x % (D / 4)) * 4, in_tile = (int)(x / (D / 4) % KEYS<D>);
-    const int64_t rest = x / (D / 4) / KEYS<D>;
+    const int c = (int)(x % (D / 4)) * 4, in_tile = (int)(x / (D / 4) % KEYS);
+    const int64_t rest = x / (D / 4) / KEYS;
     const int tile = (int)(rest % runs.kept_tiles());
     const int64_t pair = rest / runs.kept_tiles(), b = pair / p.kv_heads;
-    const int head = (int)(pair % p.kv_heads), key = tile * KEYS<D> + in_tile;
+    const int head = (int)(pair % p.kv_heads), key = tile * KEYS + in_tile;
     if (b >= p.batch || key >= p.M || runs.runs_of(tile) <= 1) return;
-    const float *from = part + ((pair * runs.kept_per_pair() + runs.slot(tile)) * 2 * KEYS<D> + in_tile) * D + c;
+    const float *from = part + ((pair * runs.kept_per_pair() + runs.slot(tile)) * 2 * KEYS + in_tile) * D + c;
     f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
-    for (int run = 0; run < runs.runs_of(tile); ++run, from += 2 * KEYS<D> * D) {
+    for (int run = 0; run < runs.runs_of(tile); ++run, from += 2 * KEYS * D) {
         dk += *(const f32x4 *)from;
-        dv += *(const f32x4 *)(from + KEYS<D> * D);
+        dv += *(const f32x4 *)(from + KEYS * D);
     }
     const float back = 1.0f / __builtin_sqrtf((float)D);
     bf16x4 u, v;
@@ -509,7 +518,7 @@ template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const W
 // tiles of sinks, which every later row sees, into runs as long as the other tiles' work.
 Runs choose_runs(const WindowProblem &p)
 {
-    const int keys = p.d == 128 ? KEYS<128> : KEYS<64>;
+    const int keys = KEYS;
     Runs r = {(p.M + keys - 1) / keys, 0, 1, 1};
     const int64_t pairs = (int64_t)p.batch * p.kv_heads;
     const int64_t usual = std::min<int64_t>(p.N, (int64_t)p.window + keys), steps = (usual + TILE - 1) / TILE * p.group;
@@ -525,9 +534,12 @@ Runs choose_runs(const WindowProblem &p)
 
 int64_t stats_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * padded_rows(p.N) * 8 + 255) / 256 * 256; }
 
+int64_t marks_bytes(const WindowProblem &p) { return (int64_t)p.batch * p.kv_heads * choose_runs(p).per_pair() * 16; }
+
 template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace, hipStream_t s)
 {
-    float *lse2 = (float *)workspace, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)((char *)workspace + stats_bytes(p));
+    float *lse2 = (float *)workspace, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)((char *)workspace + stats_bytes(p) + (p.M > 0 ? marks_bytes(p) : 0));
+    int *marks = (int *)((char *)workspace + stats_bytes(p));
     const float scale = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
     const int tiles = (int)(((int64_t)p.N * p.group + 127) / 128);
     const int64_t pairs = (int64_t)p.batch * p.kv_heads;
@@ -536,9 +548,13 @@ template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace,
     hipError_t e = hipSuccess;
     if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs)), dim3(256), s, p, tiles, scale, lse2, Ds);
     if (e != hipSuccess || p.M == 0) return e;
-    e = launch_kernel(grad_kv_kernel<D>, dim3((unsigned)(runs.per_pair() * pairs)), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part);
+    auto keys_of = [&](auto kernel) {
+        return launch_kernel(kernel, dim3((unsigned)(runs.per_pair() * pairs)), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, marks);
+    };
+    e = keys_of(grad_kv_kernel<D, false>);
+    if (e == hipSuccess) e = keys_of(grad_kv_kernel<D, true>);
     if (e != hipSuccess || runs.kept_tiles() == 0) return e;
-    const int64_t threads = pairs * runs.kept_tiles() * KEYS<D> * (D / 4);
+    const int64_t threads = pairs * runs.kept_tiles() * KEYS * (D / 4);
     return launch_kernel(grad_join_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), s, p, runs, (const float *)part);
 }
 
@@ -546,8 +562,8 @@ template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace,
 
 int64_t window_grad_workspace_bytes(const WindowProblem &p)
 {
-    const int64_t keys = p.d == 128 ? KEYS<128> : KEYS<64>;
-    return stats_bytes(p) + (p.M > 0 ? (int64_t)p.batch * p.kv_heads * choose_runs(p).kept_per_pair() * 2 * keys * p.d * 4 : 0);
+    const int64_t keys = KEYS;
+    return stats_bytes(p) + (p.M > 0 ? marks_bytes(p) + (int64_t)p.batch * p.kv_heads * choose_runs(p).kept_per_pair() * 2 * keys * p.d * 4 : 0);
 }
 
 hipError_t launch_window_grad(const WindowProblem &p, void *workspace, int64_t, hipStream_t s)
