@@ -19,7 +19,13 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 // 64 lanes x 16 bytes from global memory, an address per lane, into LDS at lds_addr + lane * 16
 __device__ __forceinline__ void copy16_from(const char *src, uint32_t lds_addr)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(src) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(src) : "memory", "m0");
+}
+
+// the same from a wave-uniform base and an offset per lane
+__device__ __forceinline__ void copy16_from(const char *base, uint32_t lane_off, uint32_t lds_addr)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(__builtin_amdgcn_readfirstlane(lds_addr)), "v"(lane_off), "s"(base) : "memory", "m0");
 }
 
 __device__ __forceinline__ i32x4 mfma_frag(i32x2 lo, i32x2 hi) { return (i32x4){lo[0], lo[1], hi[0], hi[1]}; }
@@ -77,6 +83,65 @@ __device__ __forceinline__ int finite_pair(int pair)
 {
     const unsigned u = (unsigned)pair, low = (u & 0x7f80u) == 0x7f80u ? 0 : u & 0xffffu, high = (u & 0x7f800000u) == 0x7f800000u ? 0 : u & 0xffff0000u;
     return (int)(low | high);
+}
+
+// The keys that the rows r_first .. r_last of a call see, [0, sink_end) and [lo, hi], as a list of tiles of KT keys: those of the sinks, then
+// those of the window.  Row r stands at position r / group + M - N.
+template <int KT> struct KeyList {
+    int lo, hi, sink_end, sink_tiles, window_tile, count;
+    __device__ __forceinline__ KeyList(int r_first, int r_last, int group, int N, int M, int window, int sinks)
+    {
+        const int p_first = r_first / group + M - N;
+        hi = r_last / group + M - N;
+        lo = p_first >= window ? p_first - window + 1 : 0;
+        sink_end = sinks < lo ? sinks : lo;
+        sink_tiles = (sink_end + KT - 1) / KT;
+        window_tile = lo / KT > sink_tiles ? lo / KT : sink_tiles;
+        count = hi < 0 ? 0 : sink_tiles + (hi / KT - window_tile + 1 > 0 ? hi / KT - window_tile + 1 : 0);
+    }
+    __device__ __forceinline__ int tile_key(int u) const { return (u < sink_tiles ? u : window_tile - sink_tiles + u) * KT; }
+    // a key of the list in place of one that no row sees
+    __device__ __forceinline__ int seen_key(int key) const
+    {
+        key = key < hi ? key : hi;
+        return key >= sink_end && key < lo ? lo : key;
+    }
+    __device__ __forceinline__ bool whole(int k0) const { return k0 + KT - 1 <= hi && (k0 >= lo || k0 + KT <= sink_end); }
+};
+
+// Copies of tiles of KT rows of ROW bytes into LDS by NWAVE waves: copy x of wave w moves the rows x * STEP + w * RPC .. of the tile, a lane 16
+// bytes of one of them.  swizzle(r) gives the slots of row r's chunks.
+template <int KT, int ROW, int NWAVE> struct TileCopies {
+    static constexpr int CPR = ROW / 16, RPC = 64 / CPR, STEP = NWAVE * RPC, COUNT = KT / STEP;
+    // A whole tile of dense rows: a base for all lanes and an offset each, which costs no vector instructions.  Strides below 2^25.
+    template <class Swizzle>
+    static __device__ __forceinline__ void whole(const char *rows, int64_t stride, uint32_t lds_addr, int w, int l, Swizzle &&swizzle)
+    {
+        const int row0 = w * RPC + l / CPR;
+        const uint32_t row_off = row0 * (uint32_t)stride, chunk = (l % CPR) ^ swizzle(row0);
+#pragma unroll
+        for (int x = 0; x < COUNT; ++x) copy16_from(rows + x * STEP * stride, row_off + ((chunk ^ swizzle(x * STEP)) << 4), lds_addr + (w + x * NWAVE) * 1024);
+    }
+    // row(r): the address of row r's bytes
+    template <class Row, class Swizzle>
+    static __device__ __forceinline__ void any(uint32_t lds_addr, int w, int l, Row &&row, Swizzle &&swizzle)
+    {
+#pragma unroll
+        for (int x = 0; x < COUNT; ++x) {
+            const int r = x * STEP + w * RPC + l / CPR;
+            copy16_from(row(r) + (((l % CPR) ^ swizzle(r)) << 4), lds_addr + (w + x * NWAVE) * 1024);
+        }
+    }
+};
+constexpr int64_t MOST_STRIDE = (int64_t)1 << 25;
+
+// Is there an infinity or NaN among the values that `read(i)`, i < N, yields?  0 times them is NaN, a sum that has met one stays NaN:
+// N products with zeros on matrix cores that are waiting anyway.
+template <int N, class Read> __device__ __forceinline__ bool any_infinite(Read &&read)
+{
+    f32x4 zero = {0, 0, 0, 0};
+    static_for<N>([&](auto ic) __attribute__((always_inline)) { zero = mfma16(read(ic), (i32x4){0, 0, 0, 0}, zero); });
+    return __builtin_amdgcn_ballot_w64(!(zero[0] == 0 && zero[1] == 0 && zero[2] == 0 && zero[3] == 0)) != 0;
 }
 
 }  // namespace cyc

@@ -64,11 +64,9 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     constexpr int KB = KT / 16;           // 16-key blocks per tile
     constexpr int ROW = D * 2;            // bytes per row
     constexpr int CPR = ROW / 16;         // 16-byte chunks per row: 16 (D = 128) or 8 (D = 64)
-    constexpr int RPC = 64 / CPR;         // rows per 1 KiB copy
     constexpr int DS = D / 32;            // MFMA k-steps over d
     constexpr int DT = D / 16;            // 16-wide d tiles of the output
     constexpr int TILE_BYTES = KT * ROW;
-    constexpr int COPIES = TILE_BYTES / 1024 / NWAVE;
     constexpr bool PAGED = A != DENSE;
     // LDS: two stages of the K tile, then two of the V tile; chunk c of row r sits in slot c ^ swzK(r) resp. c ^ swzV(r), so that
     // the rows that one operand read touches fall on distinct banks
@@ -137,21 +135,11 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     char *O = p.O + b * (PAGED ? 0 : p.o_batch) + (int64_t)head * group * p.o_head + (int64_t)first * p.o_row;
     const char *K = p.K + (PAGED ? 0 : b * p.k_batch) + (int64_t)head * p.k_head, *V = p.V + (PAGED ? 0 : b * p.v_batch) + (int64_t)head * p.v_head;
 
-    // ---- the keys that the rows of the workgroup see: [0, sink_end) and [lo, hi], as tiles 0 .. sink_tiles - 1 and from
-    // window_tile on; row r stands at position r / group + M - N
+    // ---- the keys that the rows of the workgroup see, and this run's share of their tiles
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
-    const int p_first = row_first / group + M - N, hi = row_last / group + M - N;
-    const int lo = p_first >= window ? p_first - window + 1 : 0;
-    const int sink_end = sinks < lo ? sinks : lo;
-    const int sink_tiles = (sink_end + KT - 1) / KT, window_tile = lo / KT > sink_tiles ? lo / KT : sink_tiles;
-    const int all_tiles = hi < 0 ? 0 : sink_tiles + (hi / KT - window_tile + 1 > 0 ? hi / KT - window_tile + 1 : 0);
-    const int u_first = (int)((int64_t)all_tiles * run / splits), ntiles = (int)((int64_t)all_tiles * (run + 1) / splits) - u_first;
-    auto tile_key = [&](int u) __attribute__((always_inline)) { return (u + u_first < sink_tiles ? u + u_first : window_tile - sink_tiles + u + u_first) * KT; };
-    // a key that some row sees in place of one that none does
-    auto seen_key = [&](int key) __attribute__((always_inline)) {
-        key = key < hi ? key : hi;
-        return key >= sink_end && key < lo ? lo : key;
-    };
+    const KeyList<KT> list(row_first, row_last, group, N, M, window, sinks);
+    const int u_first = (int)((int64_t)list.count * run / splits), ntiles = (int)((int64_t)list.count * (run + 1) / splits) - u_first;
+    auto tile_key = [&](int u) __attribute__((always_inline)) { return list.tile_key(u + u_first); };
 
     // ---- this wave's rows: first and last position, and per lane what its rows (one per 16-row block) see
     const int r0 = row_first + w * QW;
@@ -172,29 +160,53 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 #pragma unroll
         for (int ks = 0; ks < DS; ++ks) qf[jq][ks] = *(const i32x4 *)(q + ks * 64);
     }
-    // ---- copies of a tile of K and V into a stage.  Copy x of wave w moves rows x*NWAVE*RPC + w*RPC .. of the tile, lane l 16 bytes of row
-    // l / CPR of those.  Paged: every lane looks up the pages of its rows a step before it needs them.
-    const int row0 = w * RPC + l / CPR;
-    int entry[COPIES];
+    // ---- copies of a tile of K and V into a stage.  Paged: lane j looks up the page of the tile's key j a tile ahead, and a copy takes the
+    // entry of its first row, whose neighbours lie on the same page, or, at the ends of the list and in pages of a few rows, every lane that
+    // of its own row.
+    typedef TileCopies<KT, ROW, NWAVE> Copies;
+    constexpr int ENTRIES = (KT + 63) / 64;
+    int entry[ENTRIES];
+    const bool small_strides = k_row < MOST_STRIDE && v_row < MOST_STRIDE && (!PAGED || (1 << page_shift) >= Copies::RPC);
     auto look_up = [&](int u) __attribute__((always_inline)) {
-        const int k0 = tile_key(u);
+        const int k0 = tile_key(u) + l;
 #pragma unroll
-        for (int x = 0; x < COPIES; ++x) entry[x] = table[seen_key(k0 + x * (NWAVE * RPC) + row0) >> page_shift];
+        for (int x = 0; x < ENTRIES; ++x) entry[x] = table[list.seen_key(k0 + x * 64) >> page_shift];
     };
     auto issue = [&](int u) __attribute__((always_inline)) {
         const int k0 = tile_key(u);
-        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES + w * 1024;
+        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES;
+        if constexpr (PAGED) {
 #pragma unroll
-        for (int x = 0; x < COPIES; ++x) {
-            const int r = x * (NWAVE * RPC) + row0, key = seen_key(k0 + r);
-            int64_t k_off = key * k_row, v_off = key * v_row;
-            if constexpr (PAGED) {
+            for (int x = 0; x < ENTRIES; ++x) {
                 const bool outside = (unsigned)entry[x] >= (unsigned)pages;
                 bad |= outside;
-                k_off = v_off = (outside ? 0 : entry[x]) * page_bytes + (key & ((1 << page_shift) - 1)) * k_row;
+                entry[x] = outside ? 0 : entry[x];
             }
-            copy16_from(K + k_off + (((l % CPR) ^ swzK(r)) << 4), dst + x * (NWAVE * 1024));
-            copy16_from(V + v_off + (((l % CPR) ^ swzV(r)) << 4), dst + 2 * TILE_BYTES + x * (NWAVE * 1024));
+        }
+        if (small_strides && list.whole(k0)) {
+            if constexpr (!PAGED) {
+                Copies::whole(K + k0 * k_row, k_row, dst, w, l, swzK);
+                Copies::whole(V + k0 * v_row, v_row, dst + 2 * TILE_BYTES, w, l, swzV);
+            } else {
+                const int row0 = w * Copies::RPC + l / CPR;
+                const uint32_t row_off = l / CPR * (uint32_t)k_row, chunk_k = (l % CPR) ^ swzK(row0), chunk_v = (l % CPR) ^ swzV(row0);
+#pragma unroll
+                for (int x = 0; x < Copies::COUNT; ++x) {
+                    const int r = x * Copies::STEP + w * Copies::RPC;               // uniform
+                    const int page = __builtin_amdgcn_readlane(entry[x * Copies::STEP / 64], r % 64);
+                    const int64_t off = page * page_bytes + ((k0 + r) & ((1 << page_shift) - 1)) * k_row;
+                    copy16_from(K + off, row_off + ((chunk_k ^ swzK(x * Copies::STEP)) << 4), dst + (w + x * NWAVE) * 1024);
+                    copy16_from(V + off, row_off + ((chunk_v ^ swzV(x * Copies::STEP)) << 4), dst + 2 * TILE_BYTES + (w + x * NWAVE) * 1024);
+                }
+            }
+        } else {
+            auto offset = [&](int r, int64_t stride) __attribute__((always_inline)) {
+                const int key = list.seen_key(k0 + r);
+                if constexpr (!PAGED) return key * stride;
+                return __shfl(entry[r / 64 % ENTRIES], r % 64) * page_bytes + (key & ((1 << page_shift) - 1)) * k_row;
+            };
+            Copies::any(dst, w, l, [&](int r) { return K + offset(r, k_row); }, swzK);
+            Copies::any(dst + 2 * TILE_BYTES, w, l, [&](int r) { return V + offset(r, v_row); }, swzV);
         }
     };
 
@@ -333,21 +345,11 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 #pragma unroll
                 for (int r = 0; r < 4; ++r) s[ik][jq][r] = visible(k0 + 4 * g + ik * 16 + r, jq) ? s[ik][jq][r] : -__builtin_inff();
     };
-    // is there an infinity or NaN among the tile's values?
-    auto any_infinite = [&](int stage) __attribute__((always_inline)) {
-        const CYC_LDS i32x4 *v = (const CYC_LDS i32x4 *)(lds + (2 + stage) * TILE_BYTES) + l;
-        u16x2 top = {0, 0};
-#pragma unroll 4
-        for (int x = 0; x < TILE_BYTES / 1024; ++x) {
-            const i32x4 four = v[x * 64];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int word = four[r] & 0x7fff7fff;
-                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
-            }
-        }
-        const unsigned short t0 = top[0], t1 = top[1];
-        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) >= 0x7f80) != 0;
+    auto values_infinite = [&](int values) __attribute__((always_inline)) {
+        return any_infinite<TILE_BYTES / 1024>([&](auto ic) __attribute__((always_inline)) {
+            constexpr int i = decltype(ic)::value;
+            return *(const CYC_LDS i32x4 *)(lds + values + i * 1024 + l * 16);
+        });
     };
     // O^T += V^T P^T with the finite values alone, then infinities and NaNs, key by key, to the rows that see them
     auto careful_values = [&](int k0, int stage) __attribute__((always_inline)) {
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             scores();
             if (!all) {
                 mask(k0);
-                careful = any_infinite(u & 1);
+                careful = values_infinite((2 + (u & 1)) * TILE_BYTES);
             }
             weights();
             if (__builtin_expect(overflowed(), 0)) {

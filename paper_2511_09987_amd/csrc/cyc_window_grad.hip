@@ -93,21 +93,9 @@ template <int D> struct Tile {
             }
         });
     }
-    // is there an infinity or NaN in the tile?
-    static __device__ __forceinline__ bool any_infinite(const CYC_LDS char *tile, int l)
+    static __device__ __forceinline__ bool infinite(const CYC_LDS char *tile, int l)
     {
-        u16x2 top = {0, 0};
-#pragma unroll 4
-        for (int x = 0; x < TILE * ROW / 1024; ++x) {
-            const i32x4 four = ((const CYC_LDS i32x4 *)tile)[x * 64 + l];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int word = four[r] & 0x7fff7fff;
-                top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
-            }
-        }
-        const unsigned short t0 = top[0], t1 = top[1];
-        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) >= 0x7f80) != 0;
+        return any_infinite<TILE * ROW / 1024>([&](auto ic) __attribute__((always_inline)) { return ((const CYC_LDS i32x4 *)tile)[decltype(ic)::value * 64 + l]; });
     }
     // accumulate() with the finite values alone; then add(n, value) of every other value, row by row, where seen(row, n)
     template <int NB, class Seen, class Add>
@@ -167,7 +155,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
 {
     typedef Tile<D> T;
     constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, QB = 2, QW = 32, ROWS = 128;
-    constexpr int TILE_BYTES = KEY_TILE * ROW, COPIES = TILE_BYTES / 4096, RPC = 64 / CPR;
+    constexpr int TILE_BYTES = KEY_TILE * ROW;
     __shared__ __attribute__((aligned(1024))) char lds_raw[4 * TILE_BYTES];        // two stages of K, then two of V
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
@@ -181,16 +169,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
     const int64_t k_row = p.K.row, v_row = p.V.row;
 
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
-    const int p_first = row_first / group + M - N, hi = row_last / group + M - N;
-    const int lo = p_first >= window ? p_first - window + 1 : 0;
-    const int sink_end = sinks < lo ? sinks : lo;
-    const int sink_tiles = (sink_end + KEY_TILE - 1) / KEY_TILE, window_tile = lo / KEY_TILE > sink_tiles ? lo / KEY_TILE : sink_tiles;
-    const int ntiles = hi < 0 ? 0 : sink_tiles + (hi / KEY_TILE - window_tile + 1 > 0 ? hi / KEY_TILE - window_tile + 1 : 0);
-    auto tile_key = [&](int u) __attribute__((always_inline)) { return (u < sink_tiles ? u : window_tile - sink_tiles + u) * KEY_TILE; };
-    auto seen_key = [&](int key) __attribute__((always_inline)) {
-        key = key < hi ? key : hi;
-        return key >= sink_end && key < lo ? lo : key;
-    };
+    const KeyList<KEY_TILE> list(row_first, row_last, group, N, M, window, sinks);
+    const int ntiles = list.count;
 
     const int r0 = row_first + w * QW;
     const bool idle = r0 > row_last;
@@ -228,15 +208,17 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
         }
     }
 
-    const int row0 = w * RPC + l / CPR;
+    typedef TileCopies<KEY_TILE, ROW, 4> Copies;
+    const bool small_strides = k_row < MOST_STRIDE && v_row < MOST_STRIDE;
     auto issue = [&](int u) __attribute__((always_inline)) {
-        const int k0 = tile_key(u);
-        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES + w * 1024;
-#pragma unroll
-        for (int x = 0; x < COPIES; ++x) {
-            const int r = x * (4 * RPC) + row0, key = seen_key(k0 + r), chunk = ((l % CPR) ^ swizzle<CPR>(r)) << 4;
-            copy16_from(K + key * k_row + chunk, dst + x * 4096);
-            copy16_from(V + key * v_row + chunk, dst + 2 * TILE_BYTES + x * 4096);
+        const int k0 = list.tile_key(u);
+        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES;
+        if (small_strides && list.whole(k0)) {
+            Copies::whole(K + k0 * k_row, k_row, dst, w, l, swizzle<CPR>);
+            Copies::whole(V + k0 * v_row, v_row, dst + 2 * TILE_BYTES, w, l, swizzle<CPR>);
+        } else {
+            Copies::any(dst, w, l, [&](int r) { return K + list.seen_key(k0 + r) * k_row; }, swizzle<CPR>);
+            Copies::any(dst + 2 * TILE_BYTES, w, l, [&](int r) { return V + list.seen_key(k0 + r) * v_row; }, swizzle<CPR>);
         }
     };
 
@@ -252,7 +234,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
         if (u + 1 < ntiles) issue(u + 1);
 #pragma unroll 1
         for (int half = 0; half < KEY_TILE / TILE; ++half) {
-            const int k0 = tile_key(u) + half * TILE, k1 = k0 + TILE - 1;
+            const int k0 = list.tile_key(u) + half * TILE, k1 = k0 + TILE - 1;
             const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
             if (!none) {
                 const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
@@ -278,7 +260,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
                     pack<c>(y, s);
                 });
                 const CYC_LDS char *here = lds + (u & 1) * TILE_BYTES + half * TILE * ROW;
-                const bool careful = !all && T::any_infinite(here, l);
+                const bool careful = !all && T::infinite(here, l);
                 if (__builtin_expect(careful, 0)) T::accumulate_carefully(acc, by_column, here, l, y, [&](int r, int jq) { return visible(k0 + r, jq); }, not_a_number);
                 else T::template accumulate<0>(acc, by_column, y);
             }
@@ -332,7 +314,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
 {
     typedef Tile<D> T;
     constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB;
-    constexpr int TILE_BYTES = TILE * ROW, COPIES = TILE_BYTES / 1024, RPC = 64 / CPR, STAGE = 2 * TILE_BYTES + 1024;
+    constexpr int TILE_BYTES = TILE * ROW, STAGE = 2 * TILE_BYTES + 1024;
     // a stage: the tile of Q, that of dO, lse and D of its rows
     __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE];
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
@@ -342,12 +324,12 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
     if (CAREFUL && marks[at * 4] + marks[at * 4 + 1] + marks[at * 4 + 2] + marks[at * 4 + 3] == 0) return;
     bool marked = false;
-    const int per_pair = runs.per_pair(), pair = at / per_pair, slot = at - pair * per_pair;
+    const int per_pair = runs.per_pair(), pair = __builtin_amdgcn_readfirstlane(at / per_pair), slot = at - pair * per_pair;
     const int in_first = runs.first * runs.first_runs;
-    const int tile = slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs;
+    const int tile = __builtin_amdgcn_readfirstlane(slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs);
     const int run = slot - runs.slot(tile), nruns = runs.runs_of(tile);
-    const int head = pair % p.kv_heads;
-    const int64_t b = pair / p.kv_heads;
+    const int64_t b = __builtin_amdgcn_readfirstlane(pair / p.kv_heads);
+    const int head = pair - (int)b * p.kv_heads;
     const int group = p.group, N = p.N, M = p.M, window = p.window, sinks = p.sinks;
 
     // ---- the queries that see any of the keys k_first .. k_last, and this run's share of the tiles (head, 32 queries)
@@ -357,7 +339,8 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     const int i_last = k_first < sinks || reach > N - 1 ? N - 1 : (int)reach;
     const int t_first = i_first / TILE, per_head = i_last >= i_first ? i_last / TILE - t_first + 1 : 0;
     const int all_tiles = per_head * group;
-    const int u_first = (int)((int64_t)all_tiles * run / nruns), u_last = (int)((int64_t)all_tiles * (run + 1) / nruns);
+    const int u_first = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * run / nruns));
+    const int u_last = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * (run + 1) / nruns));
 
     // ---- this wave's keys as B operands
     const int kw = k_first + w * KW, kw_last = kw + KW - 1;
@@ -377,15 +360,18 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     const int64_t q_row = p.Q.row, q_head = p.Q.head, o_row = p.dO.row, o_head = p.dO.head, padded = padded_rows(N);
     const char *Q = p.Q.base + b * p.Q.batch + head * group * q_head, *dO = p.dO.base + b * p.dO.batch + head * group * o_head;
     const float *stats = (l < 32 ? lse2 : Ds) + (b * p.heads + head * group) * padded + (l & 31);
+    typedef TileCopies<TILE, ROW, 4> Copies;
+    const bool small_strides = q_row < MOST_STRIDE && o_row < MOST_STRIDE;
     auto issue = [&](int u) __attribute__((always_inline)) {
-        const int h = u / per_head, i0 = (t_first + u - h * per_head) * TILE;        // uniform
+        const int h = __builtin_amdgcn_readfirstlane(u / per_head), i0 = __builtin_amdgcn_readfirstlane((t_first + u - h * per_head) * TILE);
         const uint32_t dst = lds_base + ((u - u_first) & 1) * STAGE;
-#pragma unroll
-        for (int x = 0; x < COPIES; x += 4) {
-            // copies x .. x+3 are shared out among the four waves, one each
-            const int r = (x + w) * RPC + l / CPR, i = i0 + r < N ? i0 + r : N - 1, chunk = ((l % CPR) ^ swizzle<CPR>(r)) << 4;
-            copy16_from(Q + h * q_head + i * q_row + chunk, dst + (x + w) * 1024);
-            copy16_from(dO + h * o_head + i * o_row + chunk, dst + TILE_BYTES + (x + w) * 1024);
+        const char *q = Q + h * q_head, *o = dO + h * o_head;
+        if (small_strides && i0 + TILE <= N) {
+            Copies::whole(q + i0 * q_row, q_row, dst, w, l, swizzle<CPR>);
+            Copies::whole(o + i0 * o_row, o_row, dst + TILE_BYTES, w, l, swizzle<CPR>);
+        } else {
+            Copies::any(dst, w, l, [&](int r) { return q + (i0 + r < N ? i0 + r : N - 1) * q_row; }, swizzle<CPR>);
+            Copies::any(dst + TILE_BYTES, w, l, [&](int r) { return o + (i0 + r < N ? i0 + r : N - 1) * o_row; }, swizzle<CPR>);
         }
         if (w == 0)
             asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(dst + 2 * TILE_BYTES), "v"(stats + h * padded + i0) : "memory", "m0");
@@ -441,7 +427,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
                 pack<c>(py, s);
                 pack<c>(dsy, dp);
             });
-            const bool careful = !all && (T::any_infinite(here, l) || T::any_infinite(here + TILE_BYTES, l));
+            const bool careful = !all && (T::infinite(here, l) || T::infinite(here + TILE_BYTES, l));
             if (CAREFUL && careful) {
                 T::accumulate_carefully(dv, column_address + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
                 T::accumulate_carefully(dk, column_address, here, l, dsy, visible, not_a_number);
