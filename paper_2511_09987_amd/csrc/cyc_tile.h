@@ -16,6 +16,13 @@ typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
 #define CYC_LDS __attribute__((address_space(3)))
 
+// x, taken anew: what derives from it in a rare branch is not computed ahead of the loop and kept in registers for it
+__device__ __forceinline__ int fresh(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
 // 64 lanes x 16 bytes from global memory, an address per lane, into LDS at lds_addr + lane * 16
 __device__ __forceinline__ void copy16_from(const char *src, uint32_t lds_addr)
 {
@@ -85,10 +92,12 @@ __device__ __forceinline__ int finite_pair(int pair)
     return (int)(low | high);
 }
 
-// The keys that the rows r_first .. r_last of a call see, [0, sink_end) and [lo, hi], as a list of tiles of KT keys: those of the sinks, then
-// those of the window.  Row r stands at position r / group + M - N.
+// The keys that the rows r_first .. r_last of a call see, [0, sink_end) and [lo, hi], as a list of tiles of KT keys: first the tiles that all
+// rows see whole, then the others.  Row r stands at position r / group + M - N.
 template <int KT> struct KeyList {
-    int lo, hi, sink_end, sink_tiles, window_tile, count;
+    int lo, hi, sink_end;
+    int whole_sinks, first_whole, whole;         // whole tiles: 0 .. whole_sinks - 1, then first_whole on; `whole` of them
+    int sink_tiles, window_tile, count;          // tiles 0 .. sink_tiles - 1 and from window_tile on, whole or not
     __device__ __forceinline__ KeyList(int r_first, int r_last, int group, int N, int M, int window, int sinks)
     {
         const int p_first = r_first / group + M - N;
@@ -97,16 +106,30 @@ template <int KT> struct KeyList {
         sink_end = sinks < lo ? sinks : lo;
         sink_tiles = (sink_end + KT - 1) / KT;
         window_tile = lo / KT > sink_tiles ? lo / KT : sink_tiles;
-        count = hi < 0 ? 0 : sink_tiles + (hi / KT - window_tile + 1 > 0 ? hi / KT - window_tile + 1 : 0);
+        const int window_tiles = hi / KT - window_tile + 1 > 0 ? hi / KT - window_tile + 1 : 0;
+        count = hi < 0 ? 0 : sink_tiles + window_tiles;
+        // whole: up to the first row's position, and from the last row's window on or among the sinks
+        const int past = p_first < 0 ? 0 : (p_first + 1) / KT, last_lo = hi >= window ? hi - window + 1 : 0;
+        whole_sinks = sink_end / KT;
+        first_whole = (last_lo + KT - 1) / KT;
+        if (first_whole < window_tile) first_whole = window_tile;
+        whole = count == 0 ? 0 : whole_sinks + (past > first_whole ? past - first_whole : 0);
     }
-    __device__ __forceinline__ int tile_key(int u) const { return (u < sink_tiles ? u : window_tile - sink_tiles + u) * KT; }
+    __device__ __forceinline__ int tile_key(int u) const
+    {
+        if (u < whole) return (u < whole_sinks ? u : first_whole - whole_sinks + u) * KT;
+        u -= whole - whole_sinks;                // 0 .. sink_tiles - 1 less the whole ones, then the window's tiles less the whole ones
+        if (u < sink_tiles) return u * KT;
+        u += window_tile - sink_tiles;
+        return (u < first_whole ? u : u + whole - whole_sinks) * KT;
+    }
     // a key of the list in place of one that no row sees
     __device__ __forceinline__ int seen_key(int key) const
     {
         key = key < hi ? key : hi;
         return key >= sink_end && key < lo ? lo : key;
     }
-    __device__ __forceinline__ bool whole(int k0) const { return k0 + KT - 1 <= hi && (k0 >= lo || k0 + KT <= sink_end); }
+    __device__ __forceinline__ bool inside(int k0) const { return k0 + KT - 1 <= hi && (k0 >= lo || k0 + KT <= sink_end); }
 };
 
 // Copies of tiles of KT rows of ROW bytes into LDS by NWAVE waves: copy x of wave w moves the rows x * STEP + w * RPC .. of the tile, a lane 16
@@ -126,6 +149,7 @@ template <int KT, int ROW, int NWAVE> struct TileCopies {
     template <class Row, class Swizzle>
     static __device__ __forceinline__ void any(uint32_t lds_addr, int w, int l, Row &&row, Swizzle &&swizzle)
     {
+        l = fresh(l);
 #pragma unroll
         for (int x = 0; x < COUNT; ++x) {
             const int r = x * STEP + w * RPC + l / CPR;

@@ -61,7 +61,6 @@ template <int D, int KT, int NWAVE, int QB, Addressing A>
 __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p)
 {
     constexpr int QW = QB * 16, ROWS = NWAVE * QW;
-    constexpr int KB = KT / 16;           // 16-key blocks per tile
     constexpr int ROW = D * 2;            // bytes per row
     constexpr int CPR = ROW / 16;         // 16-byte chunks per row: 16 (D = 128) or 8 (D = 64)
     constexpr int DS = D / 32;            // MFMA k-steps over d
@@ -183,7 +182,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                 entry[x] = outside ? 0 : entry[x];
             }
         }
-        if (small_strides && list.whole(k0)) {
+        if (small_strides && list.inside(k0)) {
             if constexpr (!PAGED) {
                 Copies::whole(K + k0 * k_row, k_row, dst, w, l, swzK);
                 Copies::whole(V + k0 * v_row, v_row, dst + 2 * TILE_BYTES, w, l, swzV);
@@ -211,7 +210,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     };
 
     // ---- running state of this lane's rows: reference in the log2 domain, this lane's share of the sum, O^T accumulators
-    float m2[QB], sum[QB], tile_sum[QB];
+    float m2[QB], sum[QB], part_sum[QB];
     f32x4 acc_o[DT][QB];
 #pragma unroll
     for (int jq = 0; jq < QB; ++jq) {
@@ -220,170 +219,193 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 #pragma unroll
         for (int id = 0; id < DT; ++id) acc_o[id][jq] = (f32x4){0, 0, 0, 0};
     }
-    f32x4 s[KB][QB];                                      // S^T: [key block][row block]
-    i32x4 pf[QB][KB / 2];                                 // P^T as B operand: [row block][32-key step]
-
-    // ---- S^T = K_tile Q^T.  Fragment i = ks * KB + ik (16 keys x 32 d) feeds the QB MFMAs of key block ik and d step ks; its read is issued
-    // KWIN fragments ahead of its use and waited for on its own.  The addresses change stage from tile to tile.
-    constexpr int KWIN = 4;
-    constexpr int NFRAG = DS * KB;
-    uint32_t kaddr[DS];
-#pragma unroll
-    for (int ks = 0; ks < DS; ++ks) kaddr[ks] = lds_base + lq * ROW + (((ks * 4 + g) ^ swzK(lq)) << 4);
-    auto scores = [&]() __attribute__((always_inline)) {
-        i32x4 kf[KWIN];
-        static_for<KWIN>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            lds_read128<(i % KB) * 16 * ROW>(kf[i], kaddr[i / KB]);
-        });
-#pragma unroll
-        for (int ik = 0; ik < KB; ++ik)
-#pragma unroll
-            for (int jq = 0; jq < QB; ++jq) s[ik][jq] = (f32x4){0, 0, 0, 0};
-        static_for<NFRAG>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, ks = i / KB, ik = i % KB;
-            constexpr int later = NFRAG - 1 - i < KWIN - 1 ? NFRAG - 1 - i : KWIN - 1;   // reads issued after fragment i
-            lds_wait<later>(kf[i % KWIN]);
-#pragma unroll
-            for (int jq = 0; jq < QB; ++jq) s[ik][jq] = mfma16(kf[i % KWIN], qf[jq][ks], s[ik][jq]);
-            if constexpr (i + KWIN < NFRAG) lds_read128<((i + KWIN) % KB) * 16 * ROW>(kf[i % KWIN], kaddr[(i + KWIN) / KB]);
-        });
-    };
-
-    // ---- O^T += V^T P^T.  A operand lane: d = 16 id + l%16; k-slots 0..3 = keys 32 sk + 4 (l/16) .. +3, k-slots 4..7 = the same keys of
-    // the next 16-key block (the order P^T is packed in); two transposing reads, issued VWIN fragments ahead.
-    constexpr int VWIN = 4;
-    constexpr int NVFRAG = (KB / 2) * DT;
-    uint32_t vaddr[DT];
-#pragma unroll
-    for (int id = 0; id < DT; ++id) {
-        const int row = 4 * g + (lq >> 2);
-        const int chunk = (id * 16 + 4 * (lq & 3)) >> 3, within = ((id * 16 + 4 * (lq & 3)) & 7) * 2;
-        vaddr[id] = lds_base + 2 * TILE_BYTES + row * ROW + ((chunk ^ swzV(row)) << 4) + within;
-    }
-    auto weighted_values = [&]() __attribute__((always_inline)) {
-        i32x2 first_half[VWIN], second_half[VWIN];
-        static_for<VWIN>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, off = (i / DT) * 32 * ROW;
-            lds_read_tr64<off>(first_half[i], vaddr[i % DT]);
-            lds_read_tr64<off + 16 * ROW>(second_half[i], vaddr[i % DT]);
-        });
-        static_for<NVFRAG>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, sk = i / DT, id = i % DT;
-            constexpr int later = NVFRAG - 1 - i < VWIN - 1 ? NVFRAG - 1 - i : VWIN - 1;   // fragments requested after i
-            lds_wait2<2 * later>(first_half[i % VWIN], second_half[i % VWIN]);
-            const i32x4 vf = mfma_frag(first_half[i % VWIN], second_half[i % VWIN]);
-#pragma unroll
-            for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(vf, pf[jq][sk], acc_o[id][jq]);
-            if constexpr (i + VWIN < NVFRAG) {
-                constexpr int off = ((i + VWIN) / DT) * 32 * ROW;
-                lds_read_tr64<off>(first_half[i % VWIN], vaddr[(i + VWIN) % DT]);
-                lds_read_tr64<off + 16 * ROW>(second_half[i % VWIN], vaddr[(i + VWIN) % DT]);
-            }
-        });
-    };
+    // A tile is worked off in parts of 32 keys.
+    constexpr int PARTS = KT / 32, SF = DS * 2, VF = DT;  // of a part: fragments of K (16 keys x 32 d) and of V (32 keys x 16 d)
+    f32x4 s[2][2][QB];                                    // S^T of two parts: [part % 2][16-key block][row block]
+    i32x4 pf[2][QB];                                      // P^T as B operand: [part % 2][row block]
+    // this lane's addresses: K by rows; V transposed, k-slots 0..3 = keys 4 (l/16) .. +3 of the part, k-slots 4..7 = those 16 further on (the
+    // order P^T is packed in).  They change stage from tile to tile.
+    // 32-d step ks of K lies at kaddr ^ ks << 6, 16-d tile id of V at vaddr ^ id << 5.
+    uint32_t kaddr = lds_base + lq * ROW + ((g ^ swzK(lq)) << 4);
+    const int v_row0 = 4 * g + (lq >> 2);
+    uint32_t vaddr = lds_base + 2 * TILE_BYTES + v_row0 * ROW + ((((lq & 3) >> 1) ^ swzV(v_row0)) << 4) + (lq & 1) * 8;
 
     // ---- weights against the reference m2 (which follows the running maximum lazily, as in cyc_attn.hip), their sum, and P^T packed
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int jq = 0; jq < QB; ++jq) {
-            float part0 = 0, part1 = 0;
-#pragma unroll
-            for (int ik = 0; ik < KB; ++ik)
-#pragma unroll
-                for (int r = 0; r < 4; r += 2) {
-                    const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ik][jq][r], scale_log2e, -m2[jq]));
-                    const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[ik][jq][r + 1], scale_log2e, -m2[jq]));
-                    part0 += p0;
-                    part1 += p1;
-                    const bf16x2 pair = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
-                    pf[jq][ik >> 1][(ik & 1) * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
-                }
-            tile_sum[jq] = part0 + part1;
-        }
+    // pair X of a part: row block X / 4, 16-key block X / 2 % 2, elements X % 2 * 2 and the next
+    auto weigh_pair = [&](auto part_c, auto x_c) __attribute__((always_inline)) {
+        constexpr int P = decltype(part_c)::value, X = decltype(x_c)::value, jq = X / 4, ik = X / 2 % 2, r = X % 2 * 2;
+        const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[P][ik][jq][r], scale_log2e, -m2[jq]));
+        const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[P][ik][jq][r + 1], scale_log2e, -m2[jq]));
+        part_sum[jq] = (X % 4 == 0 ? 0.0f : part_sum[jq]) + (p0 + p1);
+        const bf16x2 pair = __builtin_convertvector((f32x2){p0, p1}, bf16x2);
+        pf[P][jq][ik * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
     };
     constexpr unsigned short LAG_BITS = 0x4380;           // 2^8 as bfloat16
-    auto overflowed = [&]() __attribute__((always_inline)) {
-        u16x2 top = {0, 0};
+    // the part's weights are all at most 2^8, after moving the reference where they were not; then they count
+    auto settle = [&](auto part_c) __attribute__((always_inline)) {
+        constexpr int P = decltype(part_c)::value;
+        u16x2 most = {0, 0};
 #pragma unroll
         for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
-            for (int sk = 0; sk < KB / 2; ++sk)
+            for (int r = 0; r < 4; ++r) {
+                const int word = pf[P][jq][r];
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, word));
+            }
+        const unsigned short t0 = most[0], t1 = most[1];
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) > LAG_BITS) != 0, 0)) {
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int word = pf[jq][sk][r];
-                    top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, word));
-                }
-        const unsigned short t0 = top[0], t1 = top[1];
-        return __builtin_amdgcn_ballot_w64((t0 > t1 ? t0 : t1) > LAG_BITS) != 0;
-    };
-    auto rebase = [&]() __attribute__((always_inline)) {
+            for (int jq = 0; jq < QB; ++jq) {
+                float top = s[P][0][jq][0];
 #pragma unroll
-        for (int jq = 0; jq < QB; ++jq) {
-            float top = s[0][jq][0];
+                for (int ik = 0; ik < 2; ++ik)
 #pragma unroll
-            for (int ik = 0; ik < KB; ++ik)
+                    for (int r = 0; r < 4; ++r) top = __builtin_fmaxf(top, s[P][ik][jq][r]);
+                // (a row that has seen nothing yet keeps a finite reference: weights 0 against it, and any score lifts it)
+                const float mh = __builtin_fmaxf(__builtin_fmaxf(m2[jq], query_max(top) * scale_log2e), -3.0e38f);
+                const float keep = __builtin_amdgcn_exp2f(m2[jq] - mh);
+                m2[jq] = mh;
+                sum[jq] *= keep;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) top = __builtin_fmaxf(top, s[ik][jq][r]);
-            // (a row that has seen nothing yet keeps a finite reference: weights 0 against it, and any score lifts it)
-            const float mh = __builtin_fmaxf(__builtin_fmaxf(m2[jq], query_max(top) * scale_log2e), -3.0e38f);
-            const float keep = __builtin_amdgcn_exp2f(m2[jq] - mh);
-            m2[jq] = mh;
-            sum[jq] *= keep;
-#pragma unroll
-            for (int id = 0; id < DT; ++id) acc_o[id][jq] *= keep;
+                for (int id = 0; id < DT; ++id) acc_o[id][jq] *= keep;
+            }
+            static_for<4 * QB>([&](auto x_c) __attribute__((always_inline)) { weigh_pair(part_c, x_c); });
         }
+#pragma unroll
+        for (int jq = 0; jq < QB; ++jq) sum[jq] += part_sum[jq];
     };
 
-    // ---- tiles that some row sees in part
-    auto visible = [&](int key, int jq) __attribute__((always_inline)) { return key <= row_hi[jq] && (key >= row_lo[jq] || key < sinks); };
-    auto mask = [&](int k0) __attribute__((always_inline)) {
-#pragma unroll
-        for (int jq = 0; jq < QB; ++jq)
-#pragma unroll
-            for (int ik = 0; ik < KB; ++ik)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) s[ik][jq][r] = visible(k0 + 4 * g + ik * 16 + r, jq) ? s[ik][jq][r] : -__builtin_inff();
+    // ---- a tile that every row of the wave sees whole.  Phase j multiplies K for part j and V for part j - 2 and takes the weights of part
+    // j - 1 in between, so that matrix and vector instructions of one wave have each other to wait for.  All fragments of the tile are one
+    // stream, whose reads run WIN fragments ahead: those of phase j are S(j) and then V(j - 2).
+    constexpr int WIN = 4, FRAGS = PARTS * (SF + VF);
+    constexpr auto phase_start = [](int j) { return (j < PARTS ? j : PARTS) * SF + (j > 2 ? j - 2 : 0) * VF; };
+    constexpr auto phase_of = [=](int f) { int j = 0; while (phase_start(j + 1) <= f) ++j; return j; };
+    constexpr auto is_k = [=](int f) { const int j = phase_of(f); return j < PARTS && f - phase_start(j) < SF; };
+    constexpr auto reads_of = [=](int first, int last) { int n = 0; for (int f = first; f <= last; ++f) n += is_k(f) ? 1 : 2; return n; };
+    i32x4 kf[WIN];
+    i32x2 va[WIN], vb[WIN];
+    auto request = [&](uint32_t k_at, uint32_t v_at, auto f_c) __attribute__((always_inline)) {
+        constexpr int f = decltype(f_c)::value;
+        if constexpr (f < FRAGS) {
+            constexpr int j = phase_of(f), i = f - phase_start(j);
+            if constexpr (is_k(f)) lds_read128<(j * 32 + i % 2 * 16) * ROW>(kf[f % WIN], k_at ^ (i / 2 << 6));
+            else {
+                constexpr int id = i - (j < PARTS ? SF : 0), off = (j - 2) * 32 * ROW;
+                lds_read_tr64<off>(va[f % WIN], v_at ^ (id << 5));
+                lds_read_tr64<off + 16 * ROW>(vb[f % WIN], v_at ^ (id << 5));
+            }
+        }
     };
-    auto values_infinite = [&](int values) __attribute__((always_inline)) {
-        return any_infinite<TILE_BYTES / 1024>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            return *(const CYC_LDS i32x4 *)(lds + values + i * 1024 + l * 16);
+    auto whole_tile = [&]() __attribute__((always_inline)) {
+        const uint32_t k_at = fresh(kaddr), v_at = fresh(vaddr);
+        static_for<WIN>([&](auto f_c) __attribute__((always_inline)) { request(k_at, v_at, f_c); });
+        static_for<PARTS + 2>([&](auto j_c) __attribute__((always_inline)) {
+            constexpr int j = decltype(j_c)::value, f0 = phase_start(j), n = phase_start(j + 1) - f0;
+            if constexpr (j < PARTS) {
+#pragma unroll
+                for (int ik = 0; ik < 2; ++ik)
+#pragma unroll
+                    for (int jq = 0; jq < QB; ++jq) s[j & 1][ik][jq] = (f32x4){0, 0, 0, 0};
+            }
+            static_for<n>([&](auto i_c) __attribute__((always_inline)) {
+                constexpr int i = decltype(i_c)::value, f = f0 + i, ahead = f + WIN - 1 < FRAGS - 1 ? f + WIN - 1 : FRAGS - 1;
+                if constexpr (is_k(f)) {
+                    lds_wait<reads_of(f + 1, ahead)>(kf[f % WIN]);
+#pragma unroll
+                    for (int jq = 0; jq < QB; ++jq) s[j & 1][i % 2][jq] = mfma16(kf[f % WIN], qf[jq][i / 2], s[j & 1][i % 2][jq]);
+                } else {
+                    constexpr int id = i - (j < PARTS ? SF : 0);
+                    lds_wait2<reads_of(f + 1, ahead)>(va[f % WIN], vb[f % WIN]);
+                    const i32x4 vf = mfma_frag(va[f % WIN], vb[f % WIN]);
+#pragma unroll
+                    for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(vf, pf[j & 1][jq], acc_o[id][jq]);
+                }
+                request(k_at, v_at, std::integral_constant<int, f + WIN>{});
+                if constexpr (j >= 1 && j <= PARTS) {
+                    constexpr int x0 = i * 4 * QB / n, x1 = (i + 1) * 4 * QB / n;
+                    static_for<x1 - x0>([&](auto x_c) __attribute__((always_inline)) {
+                        weigh_pair(std::integral_constant<int, (j - 1) & 1>{}, std::integral_constant<int, x0 + decltype(x_c)::value>{});
+                    });
+                }
+            });
+            if constexpr (j >= 1 && j <= PARTS) {
+                // (a tile of one part has nothing to put beside its weights)
+                if constexpr (n == 0) static_for<4 * QB>([&](auto x_c) __attribute__((always_inline)) { weigh_pair(std::integral_constant<int, (j - 1) & 1>{}, x_c); });
+                settle(std::integral_constant<int, (j - 1) & 1>{});
+            }
         });
     };
-    // O^T += V^T P^T with the finite values alone, then infinities and NaNs, key by key, to the rows that see them
-    auto careful_values = [&](int k0, int stage) __attribute__((always_inline)) {
+
+    // ---- any other tile, part by part
+    auto visible = [&](int key, int jq) __attribute__((always_inline)) { return (key <= row_hi[jq]) & ((key >= row_lo[jq]) | (key < sinks)); };
+    const std::integral_constant<int, 0> only;
+    auto some_of_tile = [&](int k0, int stage) __attribute__((always_inline)) {
+        const int l = fresh(threadIdx.x & 63), g = l >> 4;
+        const uint32_t k_at = fresh(kaddr), v_at = fresh(vaddr);
+#pragma unroll 1
+        for (int part = 0; part < PARTS; ++part) {
+            const int key0 = k0 + part * 32, key1 = key0 + 31, off = part * 32 * ROW;
+            if (key0 > p_hi || (key0 >= sinks && p_lo >= 0 && key1 < p_lo - window + 1)) continue;
+            const bool all = key1 <= p_lo && (key0 >= p_hi - window + 1 || key1 < sinks);
 #pragma unroll
-        for (int sk = 0; sk < KB / 2; ++sk)
+            for (int ik = 0; ik < 2; ++ik) {
 #pragma unroll
-            for (int id = 0; id < DT; ++id) {
-                i32x2 a, c;
-                asm volatile("ds_read_b64_tr_b16 %0, %2 offset:%3\n\tds_read_b64_tr_b16 %1, %2 offset:%4\n\ts_waitcnt lgkmcnt(0)"
-                             : "=&v"(a), "=&v"(c) : "v"(vaddr[id]), "n"(sk * 32 * ROW), "n"((sk * 32 + 16) * ROW));
-                const i32x4 clean = {finite_pair(a[0]), finite_pair(a[1]), finite_pair(c[0]), finite_pair(c[1])};
+                for (int jq = 0; jq < QB; ++jq) s[0][ik][jq] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(clean, pf[jq][sk], acc_o[id][jq]);
+                for (int ks = 0; ks < DS; ++ks) {
+                    const i32x4 k = *(const CYC_LDS i32x4 *)(uintptr_t)((k_at ^ ks << 6) + off + ik * 16 * ROW);
+#pragma unroll
+                    for (int jq = 0; jq < QB; ++jq) s[0][ik][jq] = mfma16(k, qf[jq][ks], s[0][ik][jq]);
+                }
             }
-        for (int key = 0; key < KT; ++key) {
-            const CYC_LDS char *row = lds + (2 + stage) * TILE_BYTES + key * ROW;
-            const int word = ((const CYC_LDS int *)row)[l % (ROW / 4)];
-            if (__builtin_amdgcn_ballot_w64(finite_pair(word) != word) == 0) continue;
-#pragma unroll
-            for (int id = 0; id < DT; ++id) {
-                const int chunk = (id * 16 + 4 * g) >> 3, within = ((id * 16 + 4 * g) & 7) * 2;
-                const bf16x4 v = *(const CYC_LDS bf16x4 *)(row + ((chunk ^ swzV(key)) << 4) + within);
+            bool careful = false;
+            if (!all) {
 #pragma unroll
                 for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (visible(k0 + key, jq) && !__builtin_isfinite((float)v[r])) acc_o[id][jq][r] += (float)v[r];
+                    for (int ik = 0; ik < 2; ++ik)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) s[0][ik][jq][r] = visible(key0 + 4 * g + ik * 16 + r, jq) ? s[0][ik][jq][r] : -__builtin_inff();
+                careful = any_infinite<32 * ROW / 1024>([&](auto ic) __attribute__((always_inline)) {
+                    constexpr int i = decltype(ic)::value;
+                    return *(const CYC_LDS i32x4 *)(lds + (2 + stage) * TILE_BYTES + off + i * 1024 + l * 16);
+                });
+            }
+            static_for<4 * QB>([&](auto x_c) __attribute__((always_inline)) { weigh_pair(only, x_c); });
+            settle(only);
+            // with finite values alone where some are not; those go, key by key, to the rows that see them
+#pragma unroll
+            for (int id = 0; id < DT; ++id) {
+                i32x2 a, c;
+                asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(a), "=&v"(c) : "v"((v_at ^ id << 5) + off), "n"(16 * ROW));
+                i32x4 vf = mfma_frag(a, c);
+                if (__builtin_expect(careful, 0)) vf = (i32x4){finite_pair(a[0]), finite_pair(a[1]), finite_pair(c[0]), finite_pair(c[1])};
+#pragma unroll
+                for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(vf, pf[0][jq], acc_o[id][jq]);
+            }
+            if (__builtin_expect(careful, 0)) {
+                for (int key = 0; key < 32; ++key) {
+                    const CYC_LDS char *row = lds + (2 + stage) * TILE_BYTES + off + key * ROW;
+                    const int word = ((const CYC_LDS int *)row)[l % (ROW / 4)];
+                    if (__builtin_amdgcn_ballot_w64(finite_pair(word) != word) == 0) continue;
+#pragma unroll
+                    for (int id = 0; id < DT; ++id) {
+                        const int chunk = (id * 16 + 4 * g) >> 3, within = ((id * 16 + 4 * g) & 7) * 2;
+                        const bf16x4 v = *(const CYC_LDS bf16x4 *)(row + ((chunk ^ swzV(key)) << 4) + within);
+#pragma unroll
+                        for (int jq = 0; jq < QB; ++jq)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) acc_o[id][jq][r] += visible(key0 + key, jq) & !__builtin_isfinite((float)v[r]) ? (float)v[r] : 0.0f;
+                    }
+                }
             }
         }
     };
 
-    // ---- One barrier per tile: tile u has landed and every wave is done with tile u-1, whose stage tile u+1 is then requested into.
-    // What a wave's tile needs it tells by scalar arithmetic.  The other workgroup on the compute unit fills the gaps between the matrix
-    // products and the vector work of a tile.
+    // ---- One barrier per tile: tile u has landed and every wave is done with tile u-1, whose stage tile u+1 is then requested into.  The
+    // tiles that all rows see whole come first, in a loop of their own: with both kinds in one, the compiler keeps a second set of
+    // accumulators.
     if (ntiles > 0) {
         if constexpr (PAGED) look_up(0);
         issue(0);
@@ -391,7 +413,8 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             if (ntiles > 1) look_up(1);
         }
     }
-    for (int u = 0; u < ntiles; ++u) {
+    int u = 0;
+    auto arrive = [&]() __attribute__((always_inline)) {
         landed_barrier();
         if (u + 1 < ntiles) {
             issue(u + 1);
@@ -399,32 +422,22 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                 if (u + 2 < ntiles) look_up(u + 2);
             }
         }
-        const int k0 = tile_key(u), k1 = k0 + KT - 1;
-        const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
-        if (!none) {
-            const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
-            bool careful = false;
-            scores();
-            if (!all) {
-                mask(k0);
-                careful = values_infinite((2 + (u & 1)) * TILE_BYTES);
-            }
-            weights();
-            if (__builtin_expect(overflowed(), 0)) {
-                rebase();
-                weights();
-            }
-#pragma unroll
-            for (int jq = 0; jq < QB; ++jq) sum[jq] += tile_sum[jq];
-            if (__builtin_expect(careful, 0)) careful_values(k0, u & 1);
-            else weighted_values();
-        }
-        // the other stage
+    };
+    auto leave = [&]() __attribute__((always_inline)) {
         const int turn = u & 1 ? -TILE_BYTES : TILE_BYTES;
-#pragma unroll
-        for (int ks = 0; ks < DS; ++ks) kaddr[ks] += turn;
-#pragma unroll
-        for (int id = 0; id < DT; ++id) vaddr[id] += turn;
+        kaddr += turn;
+        vaddr += turn;
+        ++u;
+    };
+    while (u < ntiles && u + u_first < list.whole) {
+        arrive();
+        if (!idle) whole_tile();
+        leave();
+    }
+    while (u < ntiles) {
+        arrive();
+        some_of_tile(tile_key(u), u & 1);
+        leave();
     }
 
     if constexpr (PAGED) {

@@ -122,8 +122,7 @@ template <int D> struct Tile {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        if (seen(r, n) && !__builtin_isfinite((float)v[x])) acc[id][n][x] += add((float)v[x]);
+                    for (int x = 0; x < 4; ++x) acc[id][n][x] += seen(r, n) & !__builtin_isfinite((float)v[x]) ? add((float)v[x]) : 0.0f;
             }
         }
     }
@@ -213,7 +212,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
     auto issue = [&](int u) __attribute__((always_inline)) {
         const int k0 = list.tile_key(u);
         const uint32_t dst = lds_base + (u & 1) * TILE_BYTES;
-        if (small_strides && list.whole(k0)) {
+        if (small_strides && list.inside(k0)) {
             Copies::whole(K + k0 * k_row, k_row, dst, w, l, swizzle<CPR>);
             Copies::whole(V + k0 * v_row, v_row, dst + 2 * TILE_BYTES, w, l, swizzle<CPR>);
         } else {
@@ -238,7 +237,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
             const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
             if (!none) {
                 const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
-                auto visible = [&](int key, int jq) __attribute__((always_inline)) { return key <= row_hi[jq] && (key >= row_lo[jq] || key < sinks); };
+                auto visible = [&](int key, int jq) __attribute__((always_inline)) { return (key <= row_hi[jq]) & ((key >= row_lo[jq]) | (key < sinks)); };
                 i32x4 y[QB];                                     // dS^T as B operand
                 static_for<2>([&](auto cc) __attribute__((always_inline)) {
                     constexpr int c = decltype(cc)::value;
@@ -397,7 +396,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
             asm("" : "+v"(row_address), "+v"(column_address));       // (the addresses that derive from them are cheaper taken than kept)
             auto visible = [&](int r, int n) __attribute__((always_inline)) {
                 const int position = p0 + r, key = kw + n * 16 + lq;
-                return i0 + r < N && key <= position && (position - key < window || key < sinks);
+                return (i0 + r < N) & (key <= position) & ((position - key < window) | (key < sinks));
             };
             i32x4 py[KB], dsy[KB];                                   // P and dS as B operands
             static_for<2>([&](auto cc) __attribute__((always_inline)) {
