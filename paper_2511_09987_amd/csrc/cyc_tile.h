@@ -92,6 +92,19 @@ __device__ __forceinline__ int finite_pair(int pair)
     return (int)(low | high);
 }
 
+// Which of `pairs` (batch element, key head) and which of its `units` a workgroup takes.  Workgroups go to the eight XCDs round robin by their
+// index and each XCD has its own L2: eight pairs run side by side, each on one XCD, unit after unit.  (Fewer than eight share the XCDs,
+// with neighbouring units on different ones, so that the long ones of a causal mask are spread over all.)
+struct Place {
+    int pair, unit;
+    __device__ __forceinline__ Place(int at, int pairs, int units)
+    {
+        const int base = at / (8 * units) * 8, side = pairs - base < 8 ? pairs - base : 8, local = at - base * units;
+        unit = local / side;
+        pair = base + local - unit * side;
+    }
+};
+
 // The keys that the rows r_first .. r_last of a call see, [0, sink_end) and [lo, hi], as a list of tiles of KT keys: first the tiles that all
 // rows see whole, then the others.  Row r stands at position r / group + M - N.
 template <int KT> struct KeyList {

@@ -31,9 +31,9 @@ struct TileProblem {
     int batch, kv_heads, group, N, M;                                // paged: batch = sequences, N and M by sequence
     int tiles;                                                       // tiles of rows (paged, long sequences: of all of them together)
     int tokens, pages, page_shift, max_pages, max_new, short_rows;
-    int window, sinks, splits, part_splits;
+    int window, sinks, splits, run_tiles;                            // runs of keys: how many, tiles in each
     float scale_log2e;
-    float *part, *refs;                                              // runs of keys: part[run][row][d], refs[run][row][2]
+    float *part, *refs;                                              // of the runs: part[run][row][d], refs[run][row][2]
     int64_t rows;                                                    // of all problems together
 };
 
@@ -77,27 +77,30 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4;
     const int w = NWAVE == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    // Workgroups go to the eight XCDs round robin by their linear index; renumbered, XCD x takes a contiguous range, so that
-    // the tiles of rows that read the same keys run behind one L2.
-    const int total = gridDim.x, xcd = blockIdx.x & 7;
-    int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
-    const int splits = p.splits, run = at % splits;
-    at /= splits;
-    int b, head, tile, N = p.N, M = p.M, first = 0;      // problem, key head, tile of rows; queries, keys, first token
+    const int splits = p.splits;
+    int b, head, tile, run, N = p.N, M = p.M, first = 0; // problem, key head, tile of rows, run of keys; queries, keys, first token
     bool bad = false;
     if constexpr (A == DENSE) {
         // tiles with the most keys first, the shortest last, when few workgroups are left to run beside them
-        tile = p.tiles - 1 - at % p.tiles;
-        head = at / p.tiles % p.kv_heads;
-        b = at / p.tiles / p.kv_heads;
+        const Place at(blockIdx.x, p.batch * p.kv_heads, p.tiles * splits);
+        const int t = at.unit / splits;
+        run = at.unit - t * splits;
+        tile = p.tiles - 1 - t;
+        b = at.pair / p.kv_heads;
+        head = at.pair - b * p.kv_heads;
     } else {
         if constexpr (A == PAGED_SHORT) {
-            b = at / p.kv_heads;
-            head = at % p.kv_heads;
+            // runs of one sequence and head side by side on different XCDs: nobody shares what they read
+            const int pair = blockIdx.x / splits;
+            run = blockIdx.x - pair * splits;
+            b = pair / p.kv_heads;
+            head = pair - b * p.kv_heads;
             tile = 0;
         } else {
-            const int slot = at % p.tiles;
-            head = at / p.tiles;
+            const Place at(blockIdx.x, p.kv_heads, p.tiles * splits);
+            const int slot = at.unit / splits;
+            run = at.unit - slot * splits;
+            head = at.pair;
             b = __builtin_amdgcn_readfirstlane(sequence_of_slot(p.starts, p.batch, p.tokens, p.group, ROWS, slot));
             const int start = p.starts[b];
             tile = slot - first_slot(start < 0 ? 0 : start > p.tokens ? p.tokens : start, p.group, ROWS, b);
@@ -134,10 +137,11 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     char *O = p.O + b * (PAGED ? 0 : p.o_batch) + (int64_t)head * group * p.o_head + (int64_t)first * p.o_row;
     const char *K = p.K + (PAGED ? 0 : b * p.k_batch) + (int64_t)head * p.k_head, *V = p.V + (PAGED ? 0 : b * p.v_batch) + (int64_t)head * p.v_head;
 
-    // ---- the keys that the rows of the workgroup see, and this run's share of their tiles
+    // ---- the keys that the rows of the workgroup see, and this run's share of their tiles (none, if the list ends before)
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
     const KeyList<KT> list(row_first, row_last, group, N, M, window, sinks);
-    const int u_first = (int)((int64_t)list.count * run / splits), ntiles = (int)((int64_t)list.count * (run + 1) / splits) - u_first;
+    const int u_first = run * p.run_tiles, left = list.count - u_first;
+    const int ntiles = left < p.run_tiles || run == splits - 1 ? left : p.run_tiles;
     auto tile_key = [&](int u) __attribute__((always_inline)) { return list.tile_key(u + u_first); };
 
     // ---- this wave's rows: first and last position, and per lane what its rows (one per 16-row block) see
@@ -533,75 +537,109 @@ constexpr int LONG_ROWS = 128, SHORT_ROWS = 16;
 template <int D> constexpr int LONG_KEYS = 8192 / D;
 template <int D> constexpr int SHORT_KEYS = 4096 / D;
 
-// Runs of keys for `groups` workgroups that walk up to `keys` keys each, in tiles of kt: enough to fill the chip's slots once, tiles
-// enough in each to pay for starting it.
-int choose_splits(int64_t groups, int64_t keys, int64_t kt, int64_t slots, int64_t rows, int64_t d)
+// Runs of `tiles` tiles that workgroups are cut into, each `length` of them (the last one less).
+struct Runs {
+    int count = 0, length = 0;           // count 0: no launch
+};
+Runs runs_of(int64_t tiles, int64_t want)
 {
-    int64_t splits = std::min(slots / std::max<int64_t>(groups, 1), (keys + kt - 1) / kt / 4);
-    splits = std::min<int64_t>(splits, (64 << 20) / (rows * (d + 2) * 4));
-    return (int)std::max<int64_t>(std::min<int64_t>(splits, 64), 1);
-}
-
-// keys that a row can see at most
-int64_t most_keys(int64_t keys, int window, int sinks, int64_t queries)
-{
-    return std::min<int64_t>(keys, (int64_t)window + sinks + queries);
+    tiles = std::max<int64_t>(tiles, 1);
+    const int64_t length = (tiles + want - 1) / want;
+    return {(int)((tiles + length - 1) / length), (int)length};
 }
 
 struct Mapping {
-    int short_splits, long_splits;       // 0: no launch for such sequences
+    Runs shorts, longs;                  // of sequences with up to SHORT_ROWS rows and of the others
+    int splits() const { return std::max(shorts.count, longs.count); }
 };
 
 int64_t part_bytes(int64_t rows, int64_t d, int splits) { return splits > 1 ? (rows * splits * (d + 2) * 4 + 15) / 16 * 16 : 0; }
+constexpr int64_t MOST_PART = 64 << 20;
+
+// Few rows: memory is the bound, and what is left idle at the end when sequences have different lengths.  Up to eight workgroups for each of
+// the 1280 that the chip holds, of at least eight tiles (64 x 1 token, 1000 to 8000 keys, 8 key heads: 257 us in two runs, 207 in 20).
+Runs choose_short(int64_t pairs, int64_t tiles, int64_t rows, int64_t d)
+{
+    const int64_t most = std::min<int64_t>({MOST_PART / (rows * (d + 2) * 4), tiles / 8, 10240 / std::max<int64_t>(pairs, 1), 64});
+    return runs_of(tiles, std::max<int64_t>(most, 1));
+}
+
+// Many rows: by a cost in nanoseconds.  The chip holds 512 of these workgroups, two on a compute unit, which take 1900 ns a tile of 64 keys x 128
+// rows x d 128 together, or 1050 where there is one.  More than one run adds the partial outputs, written and read at 3 TB/s, and a launch.
+Runs choose_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
+{
+    Runs best;
+    int64_t best_cost = INT64_MAX;
+    for (int64_t want = 1; want == 1 || (want * 4 <= tiles && want <= 16); ++want) {
+        const Runs r = runs_of(tiles, want);
+        const int64_t part = part_bytes(rows, d, r.count);
+        if (part > MOST_PART) break;
+        const int64_t all = groups * r.count, full = all / 512, rest = all % 512;
+        int64_t cost = (full * 1900 + (rest == 0 ? 0 : rest <= 256 ? 1050 : 1900)) * r.length;
+        if (r.count > 1) cost += 5000 + part * 2 / 3000;
+        if (cost < best_cost) {
+            best_cost = cost;
+            best = r;
+        }
+    }
+    return best;
+}
+
+// Tiles of kt keys that a workgroup's rows, `rows` of them at `queries` positions or fewer, see at most among `keys`.
+int64_t most_tiles(int64_t keys, int window, int sinks, int64_t rows, int64_t group, int64_t queries, int64_t kt)
+{
+    const int64_t span = window + std::min(queries, (rows - 1) / group + 2);
+    return std::min((keys + kt - 1) / kt, (std::min<int64_t>(span, keys) + kt - 1) / kt + 1 + (std::min<int64_t>(sinks, keys) + kt - 1) / kt);
+}
 
 Mapping window_mapping(const WindowProblem &p)
 {
-    const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads;
-    const int64_t keys = most_keys(p.M, p.window, p.sinks, p.N);
-    if (R <= SHORT_ROWS) return {choose_splits(pairs, keys, 4096 / p.d, 1280, R * pairs, p.d), 0};
-    return {0, choose_splits(pairs * ((R + LONG_ROWS - 1) / LONG_ROWS), keys, 8192 / p.d, 512, R * pairs, p.d)};
+    const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads, rows = R * pairs;
+    const bool shorts = R <= SHORT_ROWS;
+    Mapping m;
+    if (shorts) m.shorts = choose_short(pairs, most_tiles(p.M, p.window, p.sinks, SHORT_ROWS, p.group, p.N, 4096 / p.d), rows, p.d);
+    else m.longs = choose_long(pairs * ((R + LONG_ROWS - 1) / LONG_ROWS), most_tiles(p.M, p.window, p.sinks, LONG_ROWS, p.group, p.N, 8192 / p.d), rows, p.d);
+    return m;
 }
 
 int64_t long_slots(const PagedProblem &p) { return (int64_t)p.tokens * p.group / LONG_ROWS + p.seqs; }
 
 Mapping paged_mapping(const PagedProblem &p)
 {
-    const int64_t keys = most_keys((int64_t)p.max_pages << p.page_shift, p.window, p.sinks, p.max_new), rows = (int64_t)p.tokens * p.heads;
-    Mapping m = {0, 0};
+    const int64_t all = (int64_t)p.max_pages << p.page_shift, rows = (int64_t)p.tokens * p.heads;
+    auto tiles = [&](int64_t tile_rows, int64_t kt) { return most_tiles(all, p.window, p.sinks, tile_rows, p.group, p.max_new, kt); };
+    Mapping m;
     const bool longs = (int64_t)p.max_new * p.group > SHORT_ROWS;
-    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.short_splits = choose_splits((int64_t)p.seqs * p.kv_heads, keys, 4096 / p.d, 1280, rows, p.d);
-    if (longs) m.long_splits = choose_splits(long_slots(p) * p.kv_heads, keys, 8192 / p.d, 512, rows, p.d);
+    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), rows, p.d);
+    if (longs) m.longs = choose_long(long_slots(p) * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
     return m;
 }
 
 template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, const Mapping &m, hipStream_t s)
 {
     hipError_t e = hipSuccess;
-    auto launch = [&](auto kernel, int threads, int64_t groups, int splits) {
-        t.splits = splits;
-        if (groups * splits >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
-        return launch_kernel(kernel, dim3((unsigned)(groups * splits)), dim3(threads), s, t);
+    auto launch = [&](auto kernel, int threads, int64_t groups, const Runs &runs) {
+        t.splits = runs.count;
+        t.run_tiles = runs.length;
+        if (groups * runs.count >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+        return launch_kernel(kernel, dim3((unsigned)(groups * runs.count)), dim3(threads), s, t);
     };
-    if (m.short_splits) {
-        const int64_t groups = (int64_t)t.batch * t.kv_heads;
-        e = launch(tile_kernel<D, SHORT_KEYS<D>, 1, 1, PAGED ? PAGED_SHORT : DENSE>, 64, groups, m.short_splits);
-    }
-    if (e == hipSuccess && m.long_splits)
-        e = launch(tile_kernel<D, LONG_KEYS<D>, 4, 2, PAGED ? PAGED_LONG : DENSE>, 256, (int64_t)t.tiles * t.kv_heads * (PAGED ? 1 : t.batch), m.long_splits);
-    if (e != hipSuccess || std::max(m.short_splits, m.long_splits) <= 1) return e;
+    const int64_t pairs = (int64_t)t.batch * t.kv_heads;
+    if (m.shorts.count) e = launch(tile_kernel<D, SHORT_KEYS<D>, 1, 1, PAGED ? PAGED_SHORT : DENSE>, 64, pairs, m.shorts);
+    if (e == hipSuccess && m.longs.count)
+        e = launch(tile_kernel<D, LONG_KEYS<D>, 4, 2, PAGED ? PAGED_LONG : DENSE>, 256, t.tiles * (PAGED ? t.kv_heads : pairs), m.longs);
+    if (e != hipSuccess || m.splits() <= 1) return e;
     const int64_t per = 1024 / D;
-    return launch_kernel(join_kernel<D, PAGED>, dim3((unsigned)((t.rows + per - 1) / per)), dim3(256), s, t, m.short_splits, PAGED ? m.long_splits : std::max(m.short_splits, m.long_splits));
+    return launch_kernel(join_kernel<D, PAGED>, dim3((unsigned)((t.rows + per - 1) / per)), dim3(256), s, t, m.shorts.count, PAGED ? m.longs.count : m.splits());
 }
 
 void split_memory(TileProblem &t, Mapping &m, int64_t d, void *workspace, int64_t workspace_bytes)
 {
-    const int splits = std::max(m.short_splits, m.long_splits);
-    if (part_bytes(t.rows, d, splits) > workspace_bytes) {
-        m.short_splits = std::min(m.short_splits, 1);
-        m.long_splits = std::min(m.long_splits, 1);
-    }
+    if (part_bytes(t.rows, d, m.splits()) > workspace_bytes)
+        for (Runs *r : {&m.shorts, &m.longs})
+            if (r->count) *r = {1, r->count * r->length};
     t.part = (float *)workspace;
-    t.refs = t.part + t.rows * d * splits;
+    t.refs = t.part + t.rows * d * m.splits();
     t.scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
 }
 
@@ -610,7 +648,7 @@ void split_memory(TileProblem &t, Mapping &m, int64_t d, void *workspace, int64_
 int64_t window_workspace_bytes(const WindowProblem &p)
 {
     const Mapping m = window_mapping(p);
-    return part_bytes((int64_t)p.batch * p.heads * p.N, p.d, std::max(m.short_splits, m.long_splits));
+    return part_bytes((int64_t)p.batch * p.heads * p.N, p.d, m.splits());
 }
 
 hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
@@ -623,7 +661,7 @@ hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t worksp
     t.window = p.window, t.sinks = p.sinks;
     t.rows = (int64_t)p.batch * p.heads * p.N;
     Mapping m = window_mapping(p);
-    t.tiles = m.short_splits ? 1 : (int)(((int64_t)p.N * p.group + LONG_ROWS - 1) / LONG_ROWS);
+    t.tiles = m.shorts.count ? 1 : (int)(((int64_t)p.N * p.group + LONG_ROWS - 1) / LONG_ROWS);
     split_memory(t, m, p.d, workspace, workspace_bytes);
     return p.d == 128 ? launch_tiles<128, false>(t, m, s) : launch_tiles<64, false>(t, m, s);
 }
@@ -631,7 +669,7 @@ hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t worksp
 int64_t paged_workspace_bytes(const PagedProblem &p)
 {
     const Mapping m = paged_mapping(p);
-    return part_bytes((int64_t)p.tokens * p.heads, p.d, std::max(m.short_splits, m.long_splits));
+    return part_bytes((int64_t)p.tokens * p.heads, p.d, m.splits());
 }
 
 hipError_t launch_paged(const PagedProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
@@ -645,8 +683,8 @@ hipError_t launch_paged(const PagedProblem &p, void *workspace, int64_t workspac
     t.max_pages = p.max_pages, t.max_new = p.max_new, t.window = p.window, t.sinks = p.sinks;
     t.rows = (int64_t)p.tokens * p.heads;
     Mapping m = paged_mapping(p);
-    t.short_rows = m.short_splits ? SHORT_ROWS : 0;
-    t.tiles = m.long_splits ? (int)long_slots(p) : 0;
+    t.short_rows = m.shorts.count ? SHORT_ROWS : 0;
+    t.tiles = m.longs.count ? (int)long_slots(p) : 0;
     split_memory(t, m, p.d, workspace, workspace_bytes);
     return p.d == 128 ? launch_tiles<128, true>(t, m, s) : launch_tiles<64, true>(t, m, s);
 }

@@ -159,10 +159,10 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int total = gridDim.x, xcd = blockIdx.x & 7;                              // (see tile_kernel)
-    const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
-    const int tile = tiles - 1 - at % tiles, head = at / tiles % p.kv_heads;
-    const int64_t b = at / tiles / p.kv_heads;
+    const Place at(blockIdx.x, p.batch * p.kv_heads, tiles);
+    const int tile = tiles - 1 - at.unit;                                           // (the most keys first)
+    const int64_t b = at.pair / p.kv_heads;
+    const int head = at.pair - (int)b * p.kv_heads;
     const int group = p.group, N = p.N, M = p.M, R = N * group, window = p.window, sinks = p.sinks;
     const char *K = p.K.base + b * p.K.batch + head * p.K.head, *V = p.V.base + b * p.V.batch + head * p.V.head;
     const int64_t k_row = p.K.row, v_row = p.V.row;
@@ -319,11 +319,11 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int total = gridDim.x, xcd = blockIdx.x & 7;
-    const int at = xcd * (total >> 3) + (xcd < (total & 7) ? xcd : (total & 7)) + (blockIdx.x >> 3);
-    if (CAREFUL && marks[at * 4] + marks[at * 4 + 1] + marks[at * 4 + 2] + marks[at * 4 + 3] == 0) return;
+    const int mark = blockIdx.x * 4;
+    if (CAREFUL && marks[mark] + marks[mark + 1] + marks[mark + 2] + marks[mark + 3] == 0) return;
     bool marked = false;
-    const int per_pair = runs.per_pair(), pair = __builtin_amdgcn_readfirstlane(at / per_pair), slot = at - pair * per_pair;
+    const Place at(blockIdx.x, p.batch * p.kv_heads, runs.per_pair());
+    const int pair = at.pair, slot = at.unit;
     const int in_first = runs.first * runs.first_runs;
     const int tile = __builtin_amdgcn_readfirstlane(slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs);
     const int run = slot - runs.slot(tile), nruns = runs.runs_of(tile);
@@ -441,7 +441,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
         by_column += turn;
     }
 
-    if (!CAREFUL && l == 0) marks[at * 4 + w] = marked;
+    if (!CAREFUL && l == 0) marks[mark + w] = marked;
     // accumulator register r of lane l: d = 16 id + 4 (l/16) + r, key kw + 16 n + l%16
     const float back = 1.0f / __builtin_sqrtf((float)D);
 #pragma unroll
