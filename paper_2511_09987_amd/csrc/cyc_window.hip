@@ -90,9 +90,10 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
         head = at.pair - b * p.kv_heads;
     } else {
         if constexpr (A == PAGED_SHORT) {
-            // runs of one sequence and head side by side on different XCDs: nobody shares what they read
-            const int pair = blockIdx.x / splits;
-            run = blockIdx.x - pair * splits;
+            // first runs first: what the longest sequences have more than the others comes last, and on all XCDs
+            const int pairs = p.batch * p.kv_heads;
+            run = blockIdx.x / pairs;
+            const int pair = blockIdx.x - run * pairs;
             b = pair / p.kv_heads;
             head = pair - b * p.kv_heads;
             tile = 0;
@@ -163,9 +164,9 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 #pragma unroll
         for (int ks = 0; ks < DS; ++ks) qf[jq][ks] = *(const i32x4 *)(q + ks * 64);
     }
-    // ---- copies of a tile of K and V into a stage.  Paged: lane j looks up the page of the tile's key j a tile ahead, and a copy takes the
-    // entry of its first row, whose neighbours lie on the same page, or, at the ends of the list and in pages of a few rows, every lane that
-    // of its own row.
+    // ---- copies of a tile of K and V into a stage.  Paged: lane j looks up the page of the tile's key j a tile ahead and makes it the key's
+    // offset in the cache; a copy starts at that of its first row, whose neighbours lie on the same page, or, at the ends of the list and
+    // in pages of a few rows, every lane at that of its own row.
     typedef TileCopies<KT, ROW, NWAVE> Copies;
     constexpr int ENTRIES = (KT + 63) / 64;
     int entry[ENTRIES];
@@ -178,12 +179,13 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     auto issue = [&](int u) __attribute__((always_inline)) {
         const int k0 = tile_key(u);
         const uint32_t dst = lds_base + (u & 1) * TILE_BYTES;
+        int64_t at[ENTRIES];
         if constexpr (PAGED) {
 #pragma unroll
             for (int x = 0; x < ENTRIES; ++x) {
                 const bool outside = (unsigned)entry[x] >= (unsigned)pages;
                 bad |= outside;
-                entry[x] = outside ? 0 : entry[x];
+                at[x] = (outside ? 0 : entry[x]) * page_bytes + (list.seen_key(k0 + x * 64 + l) & ((1 << page_shift) - 1)) * k_row;
             }
         }
         if (small_strides && list.inside(k0)) {
@@ -195,18 +197,17 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                 const uint32_t row_off = l / CPR * (uint32_t)k_row, chunk_k = (l % CPR) ^ swzK(row0), chunk_v = (l % CPR) ^ swzV(row0);
 #pragma unroll
                 for (int x = 0; x < Copies::COUNT; ++x) {
-                    const int r = x * Copies::STEP + w * Copies::RPC;               // uniform
-                    const int page = __builtin_amdgcn_readlane(entry[x * Copies::STEP / 64], r % 64);
-                    const int64_t off = page * page_bytes + ((k0 + r) & ((1 << page_shift) - 1)) * k_row;
+                    const int r = (x * Copies::STEP + w * Copies::RPC) % 64;        // uniform
+                    const int64_t from = at[x * Copies::STEP / 64];
+                    const int64_t off = (int64_t)__builtin_amdgcn_readlane((int)(from >> 32), r) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)from, r);
                     copy16_from(K + off, row_off + ((chunk_k ^ swzK(x * Copies::STEP)) << 4), dst + (w + x * NWAVE) * 1024);
                     copy16_from(V + off, row_off + ((chunk_v ^ swzV(x * Copies::STEP)) << 4), dst + 2 * TILE_BYTES + (w + x * NWAVE) * 1024);
                 }
             }
         } else {
             auto offset = [&](int r, int64_t stride) __attribute__((always_inline)) {
-                const int key = list.seen_key(k0 + r);
-                if constexpr (!PAGED) return key * stride;
-                return __shfl(entry[r / 64 % ENTRIES], r % 64) * page_bytes + (key & ((1 << page_shift) - 1)) * k_row;
+                if constexpr (!PAGED) return list.seen_key(k0 + r) * stride;
+                return (int64_t)__shfl((int)(at[r / 64 % ENTRIES] >> 32), r % 64) << 32 | (uint32_t)__shfl((int)at[r / 64 % ENTRIES], r % 64);
             };
             Copies::any(dst, w, l, [&](int r) { return K + offset(r, k_row); }, swzK);
             Copies::any(dst + 2 * TILE_BYTES, w, l, [&](int r) { return V + offset(r, v_row); }, swzV);
@@ -556,12 +557,13 @@ struct Mapping {
 int64_t part_bytes(int64_t rows, int64_t d, int splits) { return splits > 1 ? (rows * splits * (d + 2) * 4 + 15) / 16 * 16 : 0; }
 constexpr int64_t MOST_PART = 64 << 20;
 
-// Few rows: memory is the bound, and what is left idle at the end when sequences have different lengths.  Up to eight workgroups for each of
-// the 1280 that the chip holds, of at least eight tiles (64 x 1 token, 1000 to 8000 keys, 8 key heads: 257 us in two runs, 207 in 20).
-Runs choose_short(int64_t pairs, int64_t tiles, int64_t rows, int64_t d)
+// Few rows: memory is the bound.  Keys of equal lists stream best through two workgroups on a compute unit (16 x 8 key heads x 8192 keys of
+// d 128: one run 290 us, four 97, ten 118, 32 132); sequences in pages have lengths that differ and that the host does not know, so that
+// more and shorter runs even out what the compute units get (64 x 8 key heads, 1000 to 8000 keys: two runs 247 us, six 224, twenty
+// 247).  A run has at least eight tiles, which pays for its start.
+Runs choose_short(int64_t pairs, int64_t tiles, int64_t rows, int64_t d, int64_t groups)
 {
-    const int64_t most = std::min<int64_t>({MOST_PART / (rows * (d + 2) * 4), tiles / 8, 10240 / std::max<int64_t>(pairs, 1), 64});
-    return runs_of(tiles, std::max<int64_t>(most, 1));
+    return runs_of(tiles, std::max<int64_t>(std::min<int64_t>({MOST_PART / (rows * (d + 2) * 4), tiles / 8, groups / pairs, 64}), 1));
 }
 
 // Many rows: by a cost in nanoseconds.  The chip holds 512 of these workgroups, two on a compute unit, which take 1900 ns a tile of 64 keys x 128
@@ -597,7 +599,7 @@ Mapping window_mapping(const WindowProblem &p)
     const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads, rows = R * pairs;
     const bool shorts = R <= SHORT_ROWS;
     Mapping m;
-    if (shorts) m.shorts = choose_short(pairs, most_tiles(p.M, p.window, p.sinks, SHORT_ROWS, p.group, p.N, 4096 / p.d), rows, p.d);
+    if (shorts) m.shorts = choose_short(pairs, most_tiles(p.M, p.window, p.sinks, SHORT_ROWS, p.group, p.N, 4096 / p.d), rows, p.d, 512);
     else m.longs = choose_long(pairs * ((R + LONG_ROWS - 1) / LONG_ROWS), most_tiles(p.M, p.window, p.sinks, LONG_ROWS, p.group, p.N, 8192 / p.d), rows, p.d);
     return m;
 }
@@ -610,7 +612,7 @@ Mapping paged_mapping(const PagedProblem &p)
     auto tiles = [&](int64_t tile_rows, int64_t kt) { return most_tiles(all, p.window, p.sinks, tile_rows, p.group, p.max_new, kt); };
     Mapping m;
     const bool longs = (int64_t)p.max_new * p.group > SHORT_ROWS;
-    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), rows, p.d);
+    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), rows, p.d, 3072);
     if (longs) m.longs = choose_long(long_slots(p) * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
     return m;
 }
