@@ -33,27 +33,42 @@ struct TileProblem {
     int tokens, pages, page_shift, max_pages, max_new, short_rows;
     int window, sinks, splits, run_tiles;                            // runs of keys: how many, tiles in each
     float scale_log2e;
-    float *part, *refs;                                              // of the runs: part[run][row][d], refs[run][row][2]
-    int64_t rows;                                                    // of all problems together
+    // what a run leaves: part[run][row][d], refs[run][row][2].  Rows are those of O, (token or query, head) pairs, or, in launches for few rows,
+    // SHORT_ROWS for each (problem, key head)
+    float *part, *refs;
+    int64_t part_rows, rows;                                         // rows of a run there; rows of O
 };
+constexpr int LONG_ROWS = 128, SHORT_ROWS = 16;
 
 enum Addressing { DENSE, PAGED_SHORT, PAGED_LONG };
 
-// First tile slot of sequence b among those of all sequences: sequence b has the slots from here to that of b + 1, at least as many as
-// it has tiles of `per` rows, whatever starts holds.
-__device__ __forceinline__ int first_slot(int start, int group, int per, int b) { return start * group / per + b; }
-
-// Sequence of a slot: one load and ballot for 64 sequences instead of a chain of loads.
-__device__ __forceinline__ int sequence_of_slot(const int *starts, int seqs, int tokens, int group, int per, int slot)
+// Which sequence the slot-th tile of `per` rows belongs to and which of its tiles it is, counting the tiles of all sequences with more than
+// `less` rows one after the other: 64 sequences at a time, a lane counts for one.  False behind the last.
+__device__ __forceinline__ bool sequence_of_slot(const int *starts, int seqs, int tokens, int group, int per, int less, int slot, int *seq, int *tile)
 {
-    int count = 0;
+    const int l = threadIdx.x & 63;
     for (int b0 = 0; b0 < seqs; b0 += 64) {
-        const int b = b0 + (threadIdx.x & 63);
-        int at = b < seqs ? starts[b] : 0;
-        at = at < 0 ? 0 : at > tokens ? tokens : at;
-        count += __builtin_popcountll(__builtin_amdgcn_ballot_w64(b < seqs && first_slot(at, group, per, b) <= slot));
+        const int b = b0 + l;
+        int first = b < seqs ? starts[b] : 0, end = b < seqs ? starts[b + 1] : 0;
+        first = first < 0 ? 0 : first > tokens ? tokens : first;
+        end = end < first ? first : end > tokens ? tokens : end;
+        const int rows = (end - first) * group, tiles = rows > less ? (rows + per - 1) / per : 0;
+        int upto = tiles;                                  // of the sequences b0 .. b
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int below = __shfl_up(upto, d);
+            upto += l >= d ? below : 0;
+        }
+        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > slot);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            *seq = b0 + at;
+            *tile = slot - __builtin_amdgcn_readlane(upto - tiles, at);
+            return true;
+        }
+        slot -= __builtin_amdgcn_readlane(upto, 63);
     }
-    return count > 0 ? count - 1 : 0;
+    return false;
 }
 
 // D: head dimension; KT: keys per tile; NWAVE waves of QB * 16 rows.
@@ -102,9 +117,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             const int slot = at.unit / splits;
             run = at.unit - slot * splits;
             head = at.pair;
-            b = __builtin_amdgcn_readfirstlane(sequence_of_slot(p.starts, p.batch, p.tokens, p.group, ROWS, slot));
-            const int start = p.starts[b];
-            tile = slot - first_slot(start < 0 ? 0 : start > p.tokens ? p.tokens : start, p.group, ROWS, b);
+            if (!sequence_of_slot(p.starts, p.batch, p.tokens, p.group, ROWS, p.short_rows, slot, &b, &tile)) return;
         }
         int start = p.starts[b], end = p.starts[b + 1];
         M = p.lengths[b];
@@ -126,8 +139,6 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                 }
                 return;
             }
-        } else {
-            if (N * p.group <= p.short_rows || tile < 0 || (int64_t)tile * ROWS >= (int64_t)N * p.group) return;
         }
     }
     const int group = p.group, R = N * group, window = p.window, sinks = p.sinks, pages = p.pages, page_shift = p.page_shift;
@@ -364,7 +375,12 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                     for (int jq = 0; jq < QB; ++jq) s[0][ik][jq] = mfma16(k, qf[jq][ks], s[0][ik][jq]);
                 }
             }
-            bool careful = false;
+            i32x2 a[DT], c[DT];                                       // V, on its way while the weights are taken
+            static_for<DT>([&](auto id_c) __attribute__((always_inline)) {
+                constexpr int id = decltype(id_c)::value;
+                lds_read_tr64<0>(a[id], (v_at ^ id << 5) + off);
+                lds_read_tr64<16 * ROW>(c[id], (v_at ^ id << 5) + off);
+            });
             if (!all) {
 #pragma unroll
                 for (int jq = 0; jq < QB; ++jq)
@@ -372,23 +388,26 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
                     for (int ik = 0; ik < 2; ++ik)
 #pragma unroll
                         for (int r = 0; r < 4; ++r) s[0][ik][jq][r] = visible(key0 + 4 * g + ik * 16 + r, jq) ? s[0][ik][jq][r] : -__builtin_inff();
-                careful = any_infinite<32 * ROW / 1024>([&](auto ic) __attribute__((always_inline)) {
-                    constexpr int i = decltype(ic)::value;
-                    return *(const CYC_LDS i32x4 *)(lds + (2 + stage) * TILE_BYTES + off + i * 1024 + l * 16);
-                });
             }
             static_for<4 * QB>([&](auto x_c) __attribute__((always_inline)) { weigh_pair(only, x_c); });
             settle(only);
+            static_for<DT>([&](auto id_c) __attribute__((always_inline)) {
+                constexpr int id = decltype(id_c)::value;
+                lds_wait2<2 * (DT - 1 - id)>(a[id], c[id]);
+            });
+            const bool careful = !all && any_infinite<DT>([&](auto id_c) __attribute__((always_inline)) { return mfma_frag(a[decltype(id_c)::value], c[decltype(id_c)::value]); });
             // with finite values alone where some are not; those go, key by key, to the rows that see them
+            if (__builtin_expect(careful, 0)) {
 #pragma unroll
-            for (int id = 0; id < DT; ++id) {
-                i32x2 a, c;
-                asm volatile("ds_read_b64_tr_b16 %0, %2\n\tds_read_b64_tr_b16 %1, %2 offset:%3\n\ts_waitcnt lgkmcnt(0)" : "=&v"(a), "=&v"(c) : "v"((v_at ^ id << 5) + off), "n"(16 * ROW));
-                i32x4 vf = mfma_frag(a, c);
-                if (__builtin_expect(careful, 0)) vf = (i32x4){finite_pair(a[0]), finite_pair(a[1]), finite_pair(c[0]), finite_pair(c[1])};
-#pragma unroll
-                for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(vf, pf[0][jq], acc_o[id][jq]);
+                for (int id = 0; id < DT; ++id) {
+                    a[id] = (i32x2){finite_pair(a[id][0]), finite_pair(a[id][1])};
+                    c[id] = (i32x2){finite_pair(c[id][0]), finite_pair(c[id][1])};
+                }
             }
+#pragma unroll
+            for (int id = 0; id < DT; ++id)
+#pragma unroll
+                for (int jq = 0; jq < QB; ++jq) acc_o[id][jq] = mfma16(mfma_frag(a[id], c[id]), pf[0][jq], acc_o[id][jq]);
             if (__builtin_expect(careful, 0)) {
                 for (int key = 0; key < 32; ++key) {
                     const CYC_LDS char *row = lds + (2 + stage) * TILE_BYTES + off + key * ROW;
@@ -465,8 +484,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
         if (r > row_last) continue;
         const int i = r / group, h = head * group + r - i * group;
         if (splits > 1) {
-            const int64_t row = PAGED ? (int64_t)(first + i) * (p.kv_heads * group) + h : ((int64_t)b * (p.kv_heads * group) + h) * N + i;
-            const int64_t slot = run * p.rows + row;
+            const int64_t slot = run * p.part_rows + (QB == 1 ? ((int64_t)b * p.kv_heads + head) * ROWS + r : PAGED ? (int64_t)(first + i) * (p.kv_heads * group) + h : ((int64_t)b * (p.kv_heads * group) + h) * N + i);
             if (ntiles > 0)
 #pragma unroll
                 for (int id = 0; id < DT; ++id) *(f32x4 *)(p.part + slot * D + id * 16 + 4 * g) = acc_o[id][jq];
@@ -488,20 +506,27 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 
 // Joins the runs of a row in ascending order: O = sum_x exp(m_x - m) o_x / sum_x exp(m_x - m) l_x, m the largest m_x.  One thread per four
 // d; bound by a launch and the reads of part.  A run without tiles has m_x = -inf and l_x = 0, and no o_x.
-template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(const TileProblem p, int short_splits, int long_splits)
+struct Parts {
+    const float *part, *refs;
+    int64_t rows;
+    int splits;
+};
+template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(const TileProblem p, const Parts shorts, const Parts longs)
 {
     const int64_t row = (int64_t)blockIdx.x * (1024 / D) + threadIdx.x / (D / 4);
     const int c = threadIdx.x % (D / 4) * 4, heads = p.kv_heads * p.group;
     if (row >= p.rows) return;
-    int h, i, position, splits = long_splits;
-    int64_t b = 0;
+    int h, i, position;
+    int64_t b = 0, at = row;                                          // problem; row among the parts
+    bool few;
     if constexpr (PAGED) {
         i = (int)(row / heads);
         h = (int)(row % heads);
         const int seq = sequence_of(p.starts, p.batch, i), start = p.starts[seq], end = p.starts[seq + 1], n = end - start;
         if (i < start || i >= end) return;
-        if ((int64_t)n * p.group <= p.short_rows) splits = short_splits;
-        else if (p.tiles == 0) return;                                // (no launch for it: its rows are NaN already)
+        few = (int64_t)n * p.group <= p.short_rows;
+        if (!few && longs.splits == 0) return;                        // (no launch for it: its rows are NaN already)
+        if (few) at = ((int64_t)seq * p.kv_heads + h / p.group) * SHORT_ROWS + (i - start) * p.group + h % p.group;
         position = p.lengths[seq] - end + i;
         if (start < 0 || end > p.tokens || n > p.max_new || p.lengths[seq] < 0) position = 0;
     } else {
@@ -509,20 +534,24 @@ template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(
         h = (int)(row / p.N % heads);
         b = row / p.N / heads;
         position = i + p.M - p.N;
+        few = shorts.splits > 0;
+        if (few) at = (b * p.kv_heads + h / p.group) * SHORT_ROWS + i * p.group + h % p.group;
     }
-    if (splits <= 1) return;
-    const float *ref = p.refs + row * 2, *part = p.part + row * D + c;
+    const Parts from = few ? shorts : longs;
+    if (from.splits <= 1) return;
+    const float *ref = from.refs + at * 2, *part = from.part + at * D + c;
     float m = -__builtin_inff();
-    for (int x = 0; x < splits; ++x) m = __builtin_fmaxf(m, ref[x * p.rows * 2]);
+#pragma unroll 4
+    for (int x = 0; x < from.splits; ++x) m = __builtin_fmaxf(m, ref[x * from.rows * 2]);
     f32x4 o = {0, 0, 0, 0};
     float tot = 0;
 #pragma unroll 4
-    for (int x = 0; x < splits; ++x) {
-        const f32x2 mt = *(const f32x2 *)(ref + x * p.rows * 2);
+    for (int x = 0; x < from.splits; ++x) {
+        const f32x2 mt = *(const f32x2 *)(ref + x * from.rows * 2);
         if (mt[0] == -__builtin_inff() && mt[1] == 0) continue;
         const float keep = mt[0] == m ? 1.0f : __builtin_amdgcn_exp2f(mt[0] - m);
         tot = __builtin_fmaf(keep, mt[1], tot);
-        const f32x4 v = *(const f32x4 *)(part + x * p.rows * D);
+        const f32x4 v = *(const f32x4 *)(part + x * from.rows * D);
 #pragma unroll
         for (int y = 0; y < 4; ++y) o[y] = __builtin_fmaf(keep, v[y], o[y]);
     }
@@ -534,7 +563,6 @@ template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(
     if (!PAGED && p.lse && c == 0) p.lse[row] = empty ? -__builtin_inff() : (m + __builtin_amdgcn_logf(tot)) * 0.69314718055994531f;
 }
 
-constexpr int LONG_ROWS = 128, SHORT_ROWS = 16;
 template <int D> constexpr int LONG_KEYS = 8192 / D;
 template <int D> constexpr int SHORT_KEYS = 4096 / D;
 
@@ -551,11 +579,12 @@ Runs runs_of(int64_t tiles, int64_t want)
 
 struct Mapping {
     Runs shorts, longs;                  // of sequences with up to SHORT_ROWS rows and of the others
-    int splits() const { return std::max(shorts.count, longs.count); }
+    int64_t short_rows = 0, long_rows = 0;   // rows that a run leaves of them
 };
 
 int64_t part_bytes(int64_t rows, int64_t d, int splits) { return splits > 1 ? (rows * splits * (d + 2) * 4 + 15) / 16 * 16 : 0; }
-constexpr int64_t MOST_PART = 64 << 20;
+int64_t workspace_bytes_of(const Mapping &m, int64_t d) { return part_bytes(m.short_rows, d, m.shorts.count) + part_bytes(m.long_rows, d, m.longs.count); }
+constexpr int64_t MOST_PART = 128 << 20;
 
 // Few rows: memory is the bound.  Keys of equal lists stream best through two workgroups on a compute unit (16 x 8 key heads x 8192 keys of
 // d 128: one run 290 us, four 97, ten 118, 32 132); sequences in pages have lengths that differ and that the host does not know, so that
@@ -567,18 +596,19 @@ Runs choose_short(int64_t pairs, int64_t tiles, int64_t rows, int64_t d, int64_t
 }
 
 // Many rows: by a cost in nanoseconds.  The chip holds 512 of these workgroups, two on a compute unit, which take 1900 ns a tile of 64 keys x 128
-// rows x d 128 together, or 1050 where there is one.  More than one run adds the partial outputs, written and read at 3 TB/s, and a launch.
+// rows x d 128 together, or 1050 where there is one; how many there are is an estimate for sequences in pages, so that a last round
+// counts a quarter more than what it holds and not for a whole one.  A run adds 4 us of start and, all together, a launch and the
+// partial outputs, read at 3 TB/s.
 Runs choose_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
 {
     Runs best;
     int64_t best_cost = INT64_MAX;
     for (int64_t want = 1; want == 1 || (want * 4 <= tiles && want <= 16); ++want) {
         const Runs r = runs_of(tiles, want);
-        const int64_t part = part_bytes(rows, d, r.count);
+        const int64_t part = part_bytes(rows, d, r.count), all = groups * r.count;
         if (part > MOST_PART) break;
-        const int64_t all = groups * r.count, full = all / 512, rest = all % 512;
-        int64_t cost = (full * 1900 + (rest == 0 ? 0 : rest <= 256 ? 1050 : 1900)) * r.length;
-        if (r.count > 1) cost += 5000 + part * 2 / 3000;
+        int64_t cost = all <= 256 ? 1050 * r.length + 4000 : (1900 * r.length + 4000) * std::max<int64_t>(512, all + 128) / 512;
+        if (r.count > 1) cost += 5000 + part / 3000;
         if (cost < best_cost) {
             best_cost = cost;
             best = r;
@@ -599,59 +629,62 @@ Mapping window_mapping(const WindowProblem &p)
     const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads, rows = R * pairs;
     const bool shorts = R <= SHORT_ROWS;
     Mapping m;
-    if (shorts) m.shorts = choose_short(pairs, most_tiles(p.M, p.window, p.sinks, SHORT_ROWS, p.group, p.N, 4096 / p.d), rows, p.d, 512);
+    m.short_rows = pairs * SHORT_ROWS;
+    m.long_rows = rows;
+    if (shorts) m.shorts = choose_short(pairs, most_tiles(p.M, p.window, p.sinks, SHORT_ROWS, p.group, p.N, 4096 / p.d), m.short_rows, p.d, 512);
     else m.longs = choose_long(pairs * ((R + LONG_ROWS - 1) / LONG_ROWS), most_tiles(p.M, p.window, p.sinks, LONG_ROWS, p.group, p.N, 8192 / p.d), rows, p.d);
     return m;
 }
-
-int64_t long_slots(const PagedProblem &p) { return (int64_t)p.tokens * p.group / LONG_ROWS + p.seqs; }
 
 Mapping paged_mapping(const PagedProblem &p)
 {
     const int64_t all = (int64_t)p.max_pages << p.page_shift, rows = (int64_t)p.tokens * p.heads;
     auto tiles = [&](int64_t tile_rows, int64_t kt) { return most_tiles(all, p.window, p.sinks, tile_rows, p.group, p.max_new, kt); };
     Mapping m;
+    m.short_rows = (int64_t)p.seqs * p.kv_heads * SHORT_ROWS;
+    m.long_rows = rows;
     const bool longs = (int64_t)p.max_new * p.group > SHORT_ROWS;
-    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), rows, p.d, 3072);
-    if (longs) m.longs = choose_long(long_slots(p) * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
+    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), m.short_rows, p.d, 3072);
+    if (longs) {
+        // sequences with many rows: at most as many as what the longest leaves would make; each has half a tile that is not full
+        const int64_t most = std::min<int64_t>(p.seqs, 1 + (p.tokens - p.max_new) / (SHORT_ROWS / p.group + 1));
+        m.longs = choose_long(((int64_t)p.tokens * p.group / LONG_ROWS + most / 2) * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
+    }
     return m;
 }
 
-template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, const Mapping &m, hipStream_t s)
+template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, Mapping m, void *workspace, int64_t workspace_bytes, hipStream_t s)
 {
-    hipError_t e = hipSuccess;
-    auto launch = [&](auto kernel, int threads, int64_t groups, const Runs &runs) {
+    if (workspace_bytes_of(m, D) > workspace_bytes)
+        for (Runs *r : {&m.shorts, &m.longs})
+            if (r->count) *r = {1, r->count * r->length};
+    t.scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
+    char *free = (char *)workspace;
+    auto launch = [&](auto kernel, int threads, int64_t groups, const Runs &runs, int64_t rows, Parts *parts) {
         t.splits = runs.count;
         t.run_tiles = runs.length;
+        t.part = (float *)free;
+        t.refs = t.part + rows * D * runs.count;
+        t.part_rows = rows;
+        free += part_bytes(rows, D, runs.count);
+        *parts = {t.part, t.refs, rows, runs.count};
         if (groups * runs.count >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
         return launch_kernel(kernel, dim3((unsigned)(groups * runs.count)), dim3(threads), s, t);
     };
+    hipError_t e = hipSuccess;
+    Parts shorts{}, longs{};
     const int64_t pairs = (int64_t)t.batch * t.kv_heads;
-    if (m.shorts.count) e = launch(tile_kernel<D, SHORT_KEYS<D>, 1, 1, PAGED ? PAGED_SHORT : DENSE>, 64, pairs, m.shorts);
+    if (m.shorts.count) e = launch(tile_kernel<D, SHORT_KEYS<D>, 1, 1, PAGED ? PAGED_SHORT : DENSE>, 64, pairs, m.shorts, m.short_rows, &shorts);
     if (e == hipSuccess && m.longs.count)
-        e = launch(tile_kernel<D, LONG_KEYS<D>, 4, 2, PAGED ? PAGED_LONG : DENSE>, 256, t.tiles * (PAGED ? t.kv_heads : pairs), m.longs);
-    if (e != hipSuccess || m.splits() <= 1) return e;
+        e = launch(tile_kernel<D, LONG_KEYS<D>, 4, 2, PAGED ? PAGED_LONG : DENSE>, 256, t.tiles * (PAGED ? t.kv_heads : pairs), m.longs, m.long_rows, &longs);
+    if (e != hipSuccess || std::max(shorts.splits, longs.splits) <= 1) return e;
     const int64_t per = 1024 / D;
-    return launch_kernel(join_kernel<D, PAGED>, dim3((unsigned)((t.rows + per - 1) / per)), dim3(256), s, t, m.shorts.count, PAGED ? m.longs.count : m.splits());
-}
-
-void split_memory(TileProblem &t, Mapping &m, int64_t d, void *workspace, int64_t workspace_bytes)
-{
-    if (part_bytes(t.rows, d, m.splits()) > workspace_bytes)
-        for (Runs *r : {&m.shorts, &m.longs})
-            if (r->count) *r = {1, r->count * r->length};
-    t.part = (float *)workspace;
-    t.refs = t.part + t.rows * d * m.splits();
-    t.scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)d));
+    return launch_kernel(join_kernel<D, PAGED>, dim3((unsigned)((t.rows + per - 1) / per)), dim3(256), s, t, shorts, longs);
 }
 
 }  // namespace
 
-int64_t window_workspace_bytes(const WindowProblem &p)
-{
-    const Mapping m = window_mapping(p);
-    return part_bytes((int64_t)p.batch * p.heads * p.N, p.d, m.splits());
-}
+int64_t window_workspace_bytes(const WindowProblem &p) { return workspace_bytes_of(window_mapping(p), p.d); }
 
 hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
 {
@@ -662,17 +695,12 @@ hipError_t launch_window(const WindowProblem &p, void *workspace, int64_t worksp
     t.batch = p.batch, t.kv_heads = p.kv_heads, t.group = p.group, t.N = p.N, t.M = p.M;
     t.window = p.window, t.sinks = p.sinks;
     t.rows = (int64_t)p.batch * p.heads * p.N;
-    Mapping m = window_mapping(p);
+    const Mapping m = window_mapping(p);
     t.tiles = m.shorts.count ? 1 : (int)(((int64_t)p.N * p.group + LONG_ROWS - 1) / LONG_ROWS);
-    split_memory(t, m, p.d, workspace, workspace_bytes);
-    return p.d == 128 ? launch_tiles<128, false>(t, m, s) : launch_tiles<64, false>(t, m, s);
+    return p.d == 128 ? launch_tiles<128, false>(t, m, workspace, workspace_bytes, s) : launch_tiles<64, false>(t, m, workspace, workspace_bytes, s);
 }
 
-int64_t paged_workspace_bytes(const PagedProblem &p)
-{
-    const Mapping m = paged_mapping(p);
-    return part_bytes((int64_t)p.tokens * p.heads, p.d, m.splits());
-}
+int64_t paged_workspace_bytes(const PagedProblem &p) { return workspace_bytes_of(paged_mapping(p), p.d); }
 
 hipError_t launch_paged(const PagedProblem &p, void *workspace, int64_t workspace_bytes, hipStream_t s)
 {
@@ -684,11 +712,10 @@ hipError_t launch_paged(const PagedProblem &p, void *workspace, int64_t workspac
     t.batch = p.seqs, t.kv_heads = p.kv_heads, t.group = p.group, t.tokens = p.tokens, t.pages = p.pages, t.page_shift = p.page_shift;
     t.max_pages = p.max_pages, t.max_new = p.max_new, t.window = p.window, t.sinks = p.sinks;
     t.rows = (int64_t)p.tokens * p.heads;
-    Mapping m = paged_mapping(p);
+    const Mapping m = paged_mapping(p);
     t.short_rows = m.shorts.count ? SHORT_ROWS : 0;
-    t.tiles = m.longs.count ? (int)long_slots(p) : 0;
-    split_memory(t, m, p.d, workspace, workspace_bytes);
-    return p.d == 128 ? launch_tiles<128, true>(t, m, s) : launch_tiles<64, true>(t, m, s);
+    t.tiles = m.longs.count ? (int)((int64_t)p.tokens * p.group / LONG_ROWS + p.seqs) : 0;
+    return p.d == 128 ? launch_tiles<128, true>(t, m, workspace, workspace_bytes, s) : launch_tiles<64, true>(t, m, workspace, workspace_bytes, s);
 }
 
 }  // namespace cyc
