@@ -32,10 +32,31 @@ template <int CPR> __device__ __forceinline__ constexpr int swizzle(int r)
 
 constexpr int TILE = 32;                 // rows of a tile of queries, keys of a step
 
-// What both kernels do with a tile of 32 rows in LDS.  D: head dimension.
+// Both kernels multiply in groups of four LDS reads, the reads of the next group on their way meanwhile: four fragments of rows
+// (16 bytes a lane each) or the halves of two transposed ones.
+struct Group {
+    i32x4 rows[4];
+    i32x2 columns[4];
+};
+template <int PENDING, bool COLUMNS> __device__ __forceinline__ void arrived(Group &x)
+{
+    if constexpr (COLUMNS) asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(x.columns[0]), "+v"(x.columns[1]), "+v"(x.columns[2]), "+v"(x.columns[3]) : "n"(PENDING));
+    else asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(x.rows[0]), "+v"(x.rows[1]), "+v"(x.rows[2]), "+v"(x.rows[3]) : "n"(PENDING));
+}
+
+// what is left beside products: nothing, or the elements M * COUNT / MS .. of COUNT beside product M of MS
+constexpr auto nothing = [](auto) __attribute__((always_inline)) {};
+template <int COUNT, int MS, int M, class F> __device__ __forceinline__ void share(F &&f)
+{
+    constexpr int from = M * COUNT / MS, to = (M + 1) * COUNT / MS;
+    static_for<to - from>([&](auto i_c) __attribute__((always_inline)) { f(std::integral_constant<int, from + decltype(i_c)::value>{}); });
+}
+
+// A tile of rows of D elements in LDS.
 template <int D> struct Tile {
-    static constexpr int ROW = D * 2, CPR = ROW / 16, DS = D / 32, DT = D / 16, WIN = 4;
-    // this lane's addresses within a tile: row l % 16 (chunk l / 16 of 64 bytes) and, transposed, row 4 (l / 16) + (l % 16) / 4
+    static constexpr int ROW = D * 2, CPR = ROW / 16, DS = D / 32, DT = D / 16;
+    // this lane's addresses within a tile: row l % 16 (chunk l / 16 of 64 bytes; 32-element step ks is at ^ ks << 6) and, transposed, row
+    // 4 (l / 16) + (l % 16) / 4 (16-element tile id is at ^ id << 5)
     static __device__ __forceinline__ uint32_t row_address(uint32_t base, int l)
     {
         const int lq = l & 15, g = l >> 4;
@@ -46,58 +67,61 @@ template <int D> struct Tile {
         const int lq = l & 15, g = l >> 4, row = 4 * g + (lq >> 2);
         return base + row * ROW + ((((lq & 3) >> 1) ^ swizzle<CPR>(row)) << 4) + (lq & 1) * 8;
     }
-    // first[n] and second[n] = rows 16 H .. 16 H + 15 of the tile (A operand) that lies A bytes, resp. B bytes, behind `address`, times the NB
-    // stationary operands x[n][ks], resp. y[n][ks]
-    template <int H, int A, int B, int NB>
-    static __device__ __forceinline__ void products(f32x4 (&first)[NB], f32x4 (&second)[NB], uint32_t address, const i32x4 (&x)[NB][DS], const i32x4 (&y)[NB][DS])
+    // Rows: steps 2 J and 2 J + 1 of rows 0-15 and 16-31 (x.rows: step, half).  A operand of the products along d.
+    template <int J, int OFF> static __device__ __forceinline__ void request_rows(Group &x, uint32_t address)
     {
-        constexpr int N = DS * 2;
-        i32x4 f[WIN];
-        static_for<WIN>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            lds_read128<(i < DS ? A : B) + H * 16 * ROW>(f[i], address ^ (i % DS << 6));
-        });
-#pragma unroll
-        for (int n = 0; n < NB; ++n) first[n] = second[n] = (f32x4){0, 0, 0, 0};
-        static_for<N>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value, ks = i % DS, next = i + WIN;
-            constexpr int later = N - 1 - i < WIN - 1 ? N - 1 - i : WIN - 1;
-            lds_wait<later>(f[i % WIN]);
-#pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                if constexpr (i < DS) first[n] = mfma16(f[i % WIN], x[n][ks], first[n]);
-                else second[n] = mfma16(f[i % WIN], y[n][ks], second[n]);
-            }
-            if constexpr (next < N) lds_read128<(next < DS ? A : B) + H * 16 * ROW>(f[i % WIN], address ^ (next % DS << 6));
+        static_for<4>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value;
+            lds_read128<OFF + i % 2 * 16 * ROW>(x.rows[i], address ^ (2 * J + i / 2) << 6);
         });
     }
-    // acc[id][n] += (tile)^T y[n]: A operand d 16 id + l % 16, k-slots 0..3 the rows 4 (l / 16) .. +3, k-slots 4..7 those 16 further down
+    // Columns: 16-element tiles 2 J and 2 J + 1 of 32 rows.  A operand, d 16 id + l % 16; k-slots 0..3 are the rows 4 (l / 16) .. +3, k-slots 4..7
+    // those 16 further down: the order in which accumulators of the products along d, rounded, make a B operand.
+    template <int J, int OFF> static __device__ __forceinline__ void request_columns(Group &x, uint32_t address)
+    {
+        static_for<4>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value;
+            lds_read_tr64<OFF + i % 2 * 16 * ROW>(x.columns[i], address ^ (2 * J + i / 2) << 5);
+        });
+    }
+    // The products of a group, beside(m) after the m-th: vector instructions that the matrix cores hide.
+    // out[half][n] = (rows) x[n], from zero at J = 0
+    template <int J, int NB, class Beside>
+    static __device__ __forceinline__ void multiply_rows(f32x4 (&out)[2][NB], const Group &f, const i32x4 (&x)[NB][DS], Beside &&beside)
+    {
+        static_for<4 * NB>([&](auto m_c) __attribute__((always_inline)) {
+            constexpr int m = decltype(m_c)::value, i = m / NB, n = m % NB;
+            out[i % 2][n] = mfma16(f.rows[i], x[n][2 * J + i / 2], J == 0 && i < 2 ? (f32x4){0, 0, 0, 0} : out[i % 2][n]);
+            beside(m_c);
+        });
+    }
+    // acc[id][n] += (columns) y[n]
+    template <int J, int NB, class Beside>
+    static __device__ __forceinline__ void multiply_columns(f32x4 (&acc)[DT][NB], const Group &x, const i32x4 (&y)[NB], Beside &&beside)
+    {
+        static_for<2 * NB>([&](auto m_c) __attribute__((always_inline)) {
+            constexpr int m = decltype(m_c)::value, i = m / NB, n = m % NB;
+            acc[2 * J + i][n] = mfma16(mfma_frag(x.columns[2 * i], x.columns[2 * i + 1]), y[n], acc[2 * J + i][n]);
+            beside(m_c);
+        });
+    }
+    // acc[id][n] += (tile)^T y[n] on its own
     template <int OFF, int NB> static __device__ __forceinline__ void accumulate(f32x4 (&acc)[DT][NB], uint32_t address, const i32x4 (&y)[NB])
     {
-        i32x2 a[WIN], c[WIN];
-        static_for<WIN>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            lds_read_tr64<OFF>(a[i], address ^ (i << 5));
-            lds_read_tr64<OFF + 16 * ROW>(c[i], address ^ (i << 5));
-        });
-        static_for<DT>([&](auto ic) __attribute__((always_inline)) {
-            constexpr int i = decltype(ic)::value;
-            constexpr int later = DT - 1 - i < WIN - 1 ? DT - 1 - i : WIN - 1;
-            lds_wait2<2 * later>(a[i % WIN], c[i % WIN]);
-            const i32x4 f = mfma_frag(a[i % WIN], c[i % WIN]);
-#pragma unroll
-            for (int n = 0; n < NB; ++n) acc[i][n] = mfma16(f, y[n], acc[i][n]);
-            if constexpr (i + WIN < DT) {
-                lds_read_tr64<OFF>(a[i % WIN], address ^ ((i + WIN) << 5));
-                lds_read_tr64<OFF + 16 * ROW>(c[i % WIN], address ^ ((i + WIN) << 5));
-            }
+        Group x[2];
+        request_columns<0, OFF>(x[0], address);
+        static_for<DT / 2>([&](auto j_c) __attribute__((always_inline)) {
+            constexpr int j = decltype(j_c)::value;
+            if constexpr (j + 1 < DT / 2) request_columns<j + 1, OFF>(x[(j + 1) % 2], address);
+            arrived<(j + 1 < DT / 2 ? 4 : 0), true>(x[j % 2]);
+            multiply_columns<j>(acc, x[j % 2], y, nothing);
         });
     }
     static __device__ __forceinline__ bool infinite(const CYC_LDS char *tile, int l)
     {
         return any_infinite<TILE * ROW / 1024>([&](auto ic) __attribute__((always_inline)) { return ((const CYC_LDS i32x4 *)tile)[decltype(ic)::value * 64 + l]; });
     }
-    // accumulate() with the finite values alone; then add(n, value) of every other value, row by row, where seen(row, n)
+    // accumulate() with the finite values alone; then add(value) of every other value, row by row, where seen(row, n)
     template <int NB, class Seen, class Add>
     static __device__ __forceinline__ void accumulate_carefully(f32x4 (&acc)[DT][NB], uint32_t address, const CYC_LDS char *tile, int l, const i32x4 (&y)[NB], Seen &&seen, Add &&add)
     {
@@ -128,16 +152,11 @@ template <int D> struct Tile {
     }
 };
 
-// x rounded to bfloat16 as half H of an operand of the second products
-template <int H, int NB> __device__ __forceinline__ void pack(i32x4 (&y)[NB], const f32x4 (&x)[NB])
+// two values, rounded, as one word of a B operand
+__device__ __forceinline__ int pack(float x, float y)
 {
-#pragma unroll
-    for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int r = 0; r < 4; r += 2) {
-            const bf16x2 pair = __builtin_convertvector((f32x2){x[n][r], x[n][r + 1]}, bf16x2);
-            y[n][H * 2 + (r >> 1)] = __builtin_bit_cast(int, pair);
-        }
+    const bf16x2 pair = __builtin_convertvector((f32x2){x, y}, bf16x2);
+    return __builtin_bit_cast(int, pair);
 }
 
 __device__ __forceinline__ float not_a_number(float) { return __builtin_nanf(""); }
@@ -227,48 +246,104 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
 #pragma unroll
         for (int jq = 0; jq < QB; ++jq) acc[id][jq] = (f32x4){0, 0, 0, 0};
     uint32_t by_row = T::row_address(lds_base, l), by_column = T::column_address(lds_base, l);
-    if (ntiles > 0) issue(0);
-    for (int u = 0; u < ntiles; ++u) {
-        landed_barrier();
-        if (u + 1 < ntiles) issue(u + 1);
+    f32x4 s[2][2][QB], dp[2][QB];                                    // S^T of two parts of 32 keys, dP^T of one: [16 keys][16 rows]
+    i32x4 y[2][QB];                                                  // dS^T as B operand, of two parts
+    Group x[2];
+    // 16 (key, row) pairs a lane; number e: [row block][16-key block][element]
+    auto weigh = [&](auto part_c, auto e_c) __attribute__((always_inline)) {
+        constexpr int P = decltype(part_c)::value, e = decltype(e_c)::value, jq = e / 8, ik = e / 4 % 2, r = e % 4;
+        s[P][ik][jq][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[P][ik][jq][r], scale, -lse[jq]));
+    };
+    auto slope = [&](auto part_c, auto e_c) __attribute__((always_inline)) {     // elements 2 e and 2 e + 1
+        constexpr int P = decltype(part_c)::value, e = 2 * decltype(e_c)::value, jq = e / 8, ik = e / 4 % 2, r = e % 4;
+        y[P][jq][ik * 2 + r / 2] = pack(s[P][ik][jq][r] * (dp[ik][jq][r] - Di[jq]), s[P][ik][jq][r + 1] * (dp[ik][jq][r + 1] - Di[jq]));
+    };
+    // A tile that all rows see whole, two parts of 32 keys, as one stream of groups: S(0), dP(0), S(1), dP(1), dQ(0), dQ(1).  P of a part is taken
+    // beside its dP, dS(0) beside S(1), dS(1) beside dQ(0).
+    auto whole_tile = [&]() __attribute__((always_inline)) {
+        constexpr int NS = DS / 2, NQ = DT / 2, GROUPS = 4 * NS + 2 * NQ;
+        const std::integral_constant<int, 0> one;
+        const std::integral_constant<int, 1> two;
+        const uint32_t row_at = fresh(by_row), column_at = fresh(by_column);
+        auto request = [&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            if constexpr (n < 4 * NS) T::template request_rows<n % NS, n / NS % 2 * 2 * TILE_BYTES + n / (2 * NS) * TILE * ROW>(x[n % 2], row_at);
+            else if constexpr (n < GROUPS) T::template request_columns<(n - 4 * NS) % NQ, (n - 4 * NS) / NQ * TILE * ROW>(x[n % 2], column_at);
+        };
+        request(one);
+        static_for<GROUPS>([&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            request(std::integral_constant<int, n + 1>{});
+            arrived<(n + 1 < GROUPS ? 4 : 0), (n >= 4 * NS)>(x[n % 2]);
+            if constexpr (n < 4 * NS) {
+                constexpr int phase = n / NS, j = n % NS, MS = NS * 4 * QB, part = phase / 2;
+                auto beside = [&](auto m_c) __attribute__((always_inline)) {
+                    constexpr int m = j * 4 * QB + decltype(m_c)::value;
+                    if constexpr (phase == 1 || phase == 3) share<16, MS, m>([&](auto e_c) __attribute__((always_inline)) { weigh(std::integral_constant<int, part>{}, e_c); });
+                    if constexpr (phase == 2) share<8, MS, m>([&](auto e_c) __attribute__((always_inline)) { slope(one, e_c); });
+                };
+                if constexpr (phase % 2 == 0) T::template multiply_rows<j>(s[part], x[n % 2], qf, beside);
+                else T::template multiply_rows<j>(dp, x[n % 2], of, beside);
+            } else {
+                constexpr int part = (n - 4 * NS) / NQ, j = (n - 4 * NS) % NQ, MS = NQ * 2 * QB;
+                T::template multiply_columns<j>(acc, x[n % 2], y[part], [&](auto m_c) __attribute__((always_inline)) {
+                    if constexpr (part == 0) share<8, MS, j * 2 * QB + decltype(m_c)::value>([&](auto e_c) __attribute__((always_inline)) { slope(two, e_c); });
+                });
+            }
+        });
+    };
+    auto some_of_tile = [&](int k_tile, int stage) __attribute__((always_inline)) {
+        const int l = fresh(threadIdx.x & 63), g = l >> 4;
 #pragma unroll 1
         for (int half = 0; half < KEY_TILE / TILE; ++half) {
-            const int k0 = list.tile_key(u) + half * TILE, k1 = k0 + TILE - 1;
-            const bool none = k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1);
-            if (!none) {
-                const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
-                auto visible = [&](int key, int jq) __attribute__((always_inline)) { return (key <= row_hi[jq]) & ((key >= row_lo[jq]) | (key < sinks)); };
-                i32x4 y[QB];                                     // dS^T as B operand
-                static_for<2>([&](auto cc) __attribute__((always_inline)) {
-                    constexpr int c = decltype(cc)::value;
-                    f32x4 s[QB], dp[QB];                         // S^T and dP^T: 16 keys x [16 rows]
-                    T::template products<c, 0, 2 * TILE_BYTES>(s, dp, by_row, qf, of);
+            const int k0 = k_tile + half * TILE, k1 = k0 + TILE - 1;
+            if (k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1)) continue;
+            const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
+            const uint32_t row_at = fresh(by_row) + half * TILE * ROW, column_at = fresh(by_column) + half * TILE * ROW;
+            static_for<DS>([&](auto n_c) __attribute__((always_inline)) {
+                constexpr int n = decltype(n_c)::value, j = n % (DS / 2);
+                T::template request_rows<j, n / (DS / 2) * 2 * TILE_BYTES>(x[0], row_at);
+                arrived<0, false>(x[0]);
+                if constexpr (n < DS / 2) T::template multiply_rows<j>(s[0], x[0], qf, nothing);
+                else T::template multiply_rows<j>(dp, x[0], of, nothing);
+            });
+            auto visible = [&](int key, int jq) __attribute__((always_inline)) { return (key <= row_hi[jq]) & ((key >= row_lo[jq]) | (key < sinks)); };
+            static_for<16>([&](auto e_c) __attribute__((always_inline)) {
+                constexpr int e = decltype(e_c)::value, jq = e / 8, ik = e / 4 % 2, r = e % 4;
+                weigh(std::integral_constant<int, 0>{}, e_c);
+                const float ds = s[0][ik][jq][r] * (dp[ik][jq][r] - Di[jq]);
+                s[0][ik][jq][r] = all | visible(k0 + ik * 16 + 4 * g + r, jq) ? ds : 0.0f;
+            });
 #pragma unroll
-                    for (int jq = 0; jq < QB; ++jq)
+            for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[jq][r], scale, -lse[jq]));
-                            s[jq][r] = P * (dp[jq][r] - Di[jq]);
-                        }
-                    if (!all) {
-#pragma unroll
-                        for (int jq = 0; jq < QB; ++jq)
-#pragma unroll
-                            for (int r = 0; r < 4; ++r) s[jq][r] = visible(k0 + c * 16 + 4 * g + r, jq) ? s[jq][r] : 0.0f;
-                    }
-                    pack<c>(y, s);
-                });
-                const CYC_LDS char *here = lds + (u & 1) * TILE_BYTES + half * TILE * ROW;
-                const bool careful = !all && T::infinite(here, l);
-                if (__builtin_expect(careful, 0)) T::accumulate_carefully(acc, by_column, here, l, y, [&](int r, int jq) { return visible(k0 + r, jq); }, not_a_number);
-                else T::template accumulate<0>(acc, by_column, y);
-            }
-            by_row += TILE * ROW;
-            by_column += TILE * ROW;
+                for (int i = 0; i < 4; ++i) y[0][jq][i] = pack(s[0][i / 2][jq][i % 2 * 2], s[0][i / 2][jq][i % 2 * 2 + 1]);
+            const CYC_LDS char *here = lds + stage * TILE_BYTES + half * TILE * ROW;
+            if (__builtin_expect(!all && T::infinite(here, l), 0)) T::accumulate_carefully(acc, column_at, here, l, y[0], [&](int r, int jq) __attribute__((always_inline)) { return visible(k0 + r, jq); }, not_a_number);
+            else T::template accumulate<0>(acc, column_at, y[0]);
         }
-        const int turn = u & 1 ? -2 * TILE_BYTES : 0;                                // both halves done: the other stage follows, or the first
+    };
+    if (ntiles > 0) issue(0);
+    int u = 0;
+    auto arrive = [&]() __attribute__((always_inline)) {
+        landed_barrier();
+        if (u + 1 < ntiles) issue(u + 1);
+    };
+    auto leave = [&]() __attribute__((always_inline)) {
+        const int turn = u & 1 ? -TILE_BYTES : TILE_BYTES;
         by_row += turn;
         by_column += turn;
+        ++u;
+    };
+    while (u < list.whole) {                                         // (see tile_kernel: a loop for each kind of tile)
+        arrive();
+        if (!idle) whole_tile();
+        leave();
+    }
+    while (u < ntiles) {
+        arrive();
+        some_of_tile(list.tile_key(u), u & 1);
+        leave();
     }
 
     const float back = 1.0f / __builtin_sqrtf((float)D);
@@ -315,7 +390,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB;
     constexpr int TILE_BYTES = TILE * ROW, STAGE = 2 * TILE_BYTES + 1024;
     // a stage: the tile of Q, that of dO, lse and D of its rows
-    __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE];
+    __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE + KEYS * ROW];
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -331,29 +406,68 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     const int head = pair - (int)b * p.kv_heads;
     const int group = p.group, N = p.N, M = p.M, window = p.window, sinks = p.sinks;
 
-    // ---- the queries that see any of the keys k_first .. k_last, and this run's share of the tiles (head, 32 queries)
-    const int k_first = tile * KEYS, k_last = (M - k_first < KEYS ? M : k_first + KEYS) - 1;
-    const int i_first = k_first - (M - N) > 0 ? k_first - (M - N) : 0;
-    const int64_t reach = (int64_t)k_last + window - 1 - (M - N);
+    // ---- the queries that see any of the keys k_first .. k_last, as tiles (head, 32 queries): first those whose queries all see all keys of the
+    // workgroup, head by head, then the others; this run's share of them
+    const int shift = M - N, k_first = tile * KEYS, k_last = (M - k_first < KEYS ? M : k_first + KEYS) - 1;
+    const int i_first = k_first > shift ? k_first - shift : 0;
+    const int64_t reach = (int64_t)k_last + window - 1 - shift;
     const int i_last = k_first < sinks || reach > N - 1 ? N - 1 : (int)reach;
-    const int t_first = i_first / TILE, per_head = i_last >= i_first ? i_last / TILE - t_first + 1 : 0;
-    const int all_tiles = per_head * group;
+    const int t_first = i_first / TILE, t_last = i_last >= i_first ? i_last / TILE : t_first - 1, per_head = t_last - t_first + 1;
+    const int all_from = k_first + KEYS - 1 - shift > 0 ? (k_first + KEYS - 1 - shift + TILE - 1) / TILE : 0;
+    const int64_t all_reach = (int64_t)k_first + window - TILE - shift;                              // the last tile's first query
+    const int all_to = k_first + KEYS <= sinks || all_reach >= N ? N / TILE : all_reach < 0 ? 0 : min((int)(all_reach / TILE) + 1, N / TILE);
+    const int w_first = all_from > t_first ? all_from : t_first;
+    const int whole = CAREFUL || k_first + KEYS > M || all_to <= w_first ? 0 : all_to - w_first;     // of a head
+    const int others = per_head - whole, all_tiles = per_head * group, whole_tiles = whole * group;
+    const int o_first = whole > 0 && w_first == t_first ? w_first + whole : t_first;
     const int u_first = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * run / nruns));
     const int u_last = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * (run + 1) / nruns));
+    int next_head, next_tile;                                        // of the tile to be requested next
+    if (u_first < whole_tiles) {
+        next_head = u_first / whole;
+        next_tile = w_first + u_first - next_head * whole;
+    } else {
+        const int v = u_first - whole_tiles;
+        next_head = others > 0 ? v / others : 0;
+        next_tile = t_first + v - next_head * others;
+        if (whole > 0 && next_tile >= w_first) next_tile += whole;
+    }
+    next_head = __builtin_amdgcn_readfirstlane(next_head);
+    next_tile = __builtin_amdgcn_readfirstlane(next_tile);
+    auto advance = [&](int u) __attribute__((always_inline)) {        // from tile u to u + 1
+        ++next_tile;
+        if (u < whole_tiles) {
+            if (next_tile == w_first + whole) {
+                ++next_head;
+                next_tile = w_first;
+                if (u + 1 == whole_tiles) {
+                    next_head = 0;
+                    next_tile = o_first;
+                }
+            }
+        } else {
+            if (whole > 0 && next_tile == w_first) next_tile += whole;
+            if (next_tile > t_last) {
+                ++next_head;
+                next_tile = o_first;
+            }
+        }
+    };
 
-    // ---- this wave's keys as B operands
+    // ---- this wave's keys: K as B operands in registers, V, for which those do not suffice at d = 128, in LDS behind the two stages
     const int kw = k_first + w * KW, kw_last = kw + KW - 1;
-    i32x4 kf[KB][DS], vf[KB][DS];
+    i32x4 kf[KB][DS];
 #pragma unroll
     for (int n = 0; n < KB; ++n) {
         int key = kw + n * 16 + lq;
         key = key < M ? key : M - 1;
-        const char *k = p.K.base + b * p.K.batch + head * p.K.head + key * p.K.row + g * 16, *v = p.V.base + b * p.V.batch + head * p.V.head + key * p.V.row + g * 16;
+        const char *k = p.K.base + b * p.K.batch + head * p.K.head + key * p.K.row + g * 16;
 #pragma unroll
-        for (int ks = 0; ks < DS; ++ks) {
-            kf[n][ks] = *(const i32x4 *)(k + ks * 64);
-            vf[n][ks] = *(const i32x4 *)(v + ks * 64);
-        }
+        for (int ks = 0; ks < DS; ++ks) kf[n][ks] = *(const i32x4 *)(k + ks * 64);
+    }
+    {
+        const char *V = p.V.base + b * p.V.batch + head * p.V.head;
+        TileCopies<KW, ROW, 1>::any(lds_base + 2 * STAGE + w * KW * ROW, 0, l, [&](int r) { return V + (kw + r < M ? kw + r : M - 1) * p.V.row; }, swizzle<CPR>);
     }
 
     const int64_t q_row = p.Q.row, q_head = p.Q.head, o_row = p.dO.row, o_head = p.dO.head, padded = padded_rows(N);
@@ -362,9 +476,9 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     typedef TileCopies<TILE, ROW, 4> Copies;
     const bool small_strides = q_row < MOST_STRIDE && o_row < MOST_STRIDE;
     auto issue = [&](int u) __attribute__((always_inline)) {
-        const int h = __builtin_amdgcn_readfirstlane(u / per_head), i0 = __builtin_amdgcn_readfirstlane((t_first + u - h * per_head) * TILE);
+        const int i0 = next_tile * TILE;
         const uint32_t dst = lds_base + ((u - u_first) & 1) * STAGE;
-        const char *q = Q + h * q_head, *o = dO + h * o_head;
+        const char *q = Q + next_head * q_head, *o = dO + next_head * o_head;
         if (small_strides && i0 + TILE <= N) {
             Copies::whole(q + i0 * q_row, q_row, dst, w, l, swizzle<CPR>);
             Copies::whole(o + i0 * o_row, o_row, dst + TILE_BYTES, w, l, swizzle<CPR>);
@@ -373,7 +487,8 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
             Copies::any(dst + TILE_BYTES, w, l, [&](int r) { return o + (i0 + r < N ? i0 + r : N - 1) * o_row; }, swizzle<CPR>);
         }
         if (w == 0)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" : : "s"(dst + 2 * TILE_BYTES), "v"(stats + h * padded + i0) : "memory", "m0");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
+                         : : "s"(__builtin_amdgcn_readfirstlane(dst + 2 * TILE_BYTES)), "v"(stats + next_head * padded + i0) : "memory", "m0");
     };
 
     f32x4 dk[DT][KB], dv[DT][KB];
@@ -382,63 +497,139 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
 #pragma unroll
         for (int n = 0; n < KB; ++n) dk[id][n] = dv[id][n] = (f32x4){0, 0, 0, 0};
     uint32_t by_row = T::row_address(lds_base, l), by_column = T::column_address(lds_base, l);
-    if (u_first < u_last) issue(u_first);
-    for (int u = u_first; u < u_last; ++u) {
-        landed_barrier();
-        if (u + 1 < u_last) issue(u + 1);
-        const int stage = (u - u_first) & 1, i0 = (t_first + u % per_head) * TILE;
-        const int p0 = i0 + M - N, p1 = (i0 + TILE < N ? i0 + TILE : N) - 1 + M - N;
-        const bool none = kw >= M || p1 < kw || (kw >= sinks && (int64_t)p0 - kw_last >= window);
-        if (!none) {
-            const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
-            const CYC_LDS char *here = lds + stage * STAGE;
-            uint32_t row_address = by_row, column_address = by_column;
-            asm("" : "+v"(row_address), "+v"(column_address));       // (the addresses that derive from them are cheaper taken than kept)
-            auto visible = [&](int r, int n) __attribute__((always_inline)) {
-                const int position = p0 + r, key = kw + n * 16 + lq;
-                return (i0 + r < N) & (key <= position) & ((position - key < window) | (key < sinks));
-            };
-            i32x4 py[KB], dsy[KB];                                   // P and dS as B operands
-            static_for<2>([&](auto cc) __attribute__((always_inline)) {
-                constexpr int c = decltype(cc)::value;
-                f32x4 s[KB], dp[KB];                                 // S and dP: 16 queries x [16 keys]
-                T::template products<c, 0, TILE_BYTES>(s, dp, row_address, kf, vf);
-                const f32x4 lse = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + (c * 16 + 4 * g) * 4);
-                const f32x4 Di = *(const CYC_LDS f32x4 *)(here + 2 * TILE_BYTES + 128 + (c * 16 + 4 * g) * 4);
+    f32x4 s[2][KB], dp[2][KB];                                       // S and dP: [16 queries][16 keys]
+    f32x4 lse[2], Di[2];
+    i32x4 py[KB], dsy[KB];                                           // P and dS as B operands
+    Group x[2];
+    // 16 (query, key) pairs a lane; number e: [16-query block][key block][element]
+    auto weigh = [&](auto e_c) __attribute__((always_inline)) {
+        constexpr int e = decltype(e_c)::value, c = e / 8, n = e / 4 % 2, r = e % 4;
+        s[c][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], scale, -lse[c][r]));
+        if constexpr (r % 2 == 1) py[n][c * 2 + r / 2] = pack(s[c][n][r - 1], s[c][n][r]);
+    };
+    auto slope = [&](auto e_c) __attribute__((always_inline)) {       // elements 2 e and 2 e + 1
+        constexpr int e = 2 * decltype(e_c)::value, c = e / 8, n = e / 4 % 2, r = e % 4;
+        dsy[n][c * 2 + r / 2] = pack(s[c][n][r] * (dp[c][n][r] - Di[c][r]), s[c][n][r + 1] * (dp[c][n][r + 1] - Di[c][r + 1]));
+    };
+    auto read_stats = [&](f32x4(&to)[2], const CYC_LDS char *from) __attribute__((always_inline)) {
 #pragma unroll
-                for (int n = 0; n < KB; ++n)
+        for (int c = 0; c < 2; ++c) to[c] = *(const CYC_LDS f32x4 *)(from + (c * 16 + 4 * g) * 4);
+    };
+    // step ks of dO's two halves and of V's two key blocks, and their four products
+    auto request_values = [&](auto ks_c, Group &to, uint32_t row_at, uint32_t v_at) __attribute__((always_inline)) {
+        constexpr int ks = decltype(ks_c)::value;
+        lds_read128<TILE_BYTES>(to.rows[0], row_at ^ ks << 6);
+        lds_read128<TILE_BYTES + 16 * ROW>(to.rows[1], row_at ^ ks << 6);
+        lds_read128<0>(to.rows[2], v_at ^ ks << 6);
+        lds_read128<16 * ROW>(to.rows[3], v_at ^ ks << 6);
+    };
+    auto multiply_values = [&](auto ks_c, const Group &f, auto &&beside) __attribute__((always_inline)) {
+        constexpr int ks = decltype(ks_c)::value;
+        static_for<4>([&](auto m_c) __attribute__((always_inline)) {
+            constexpr int m = decltype(m_c)::value, c = m / 2, n = m % 2;
+            dp[c][n] = mfma16(f.rows[c], f.rows[2 + n], ks == 0 ? (f32x4){0, 0, 0, 0} : dp[c][n]);
+            beside(m_c);
+        });
+    };
+    const uint32_t values = T::row_address(lds_base + 2 * STAGE + w * KW * ROW, l);
+    // A tile whose queries all see all keys, as one stream of groups: S, dP beside which P is taken, dV beside which dS is, dK.
+    auto whole_tile = [&](const CYC_LDS char *here) __attribute__((always_inline)) {
+        constexpr int NS = DS / 2, NQ = DT / 2, GROUPS = NS + DS + 2 * NQ;
+        const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
+        auto request = [&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            if constexpr (n < NS) T::template request_rows<n, 0>(x[n % 2], row_at);
+            else if constexpr (n < NS + DS) request_values(std::integral_constant<int, n - NS>{}, x[n % 2], row_at, v_at);
+            else if constexpr (n < GROUPS) T::template request_columns<(n - NS - DS) % NQ, n - NS - DS < NQ ? TILE_BYTES : 0>(x[n % 2], column_at);
+        };
+        request(std::integral_constant<int, 0>{});
+        static_for<GROUPS>([&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            if constexpr (n == NS - 1) read_stats(lse, here + 2 * TILE_BYTES);
+            if constexpr (n == NS + DS - 1) read_stats(Di, here + 2 * TILE_BYTES + 128);
+            request(std::integral_constant<int, n + 1>{});
+            arrived<(n + 1 < GROUPS ? 4 : 0), (n >= NS + DS)>(x[n % 2]);
+            if constexpr (n < NS) T::template multiply_rows<n>(s, x[n % 2], kf, nothing);
+            else if constexpr (n < NS + DS) {
+                multiply_values(std::integral_constant<int, n - NS>{}, x[n % 2], [&](auto m_c) __attribute__((always_inline)) {
+                    share<16, 4 * DS, (n - NS) * 4 + decltype(m_c)::value>(weigh);
+                });
+            } else if constexpr (n < NS + DS + NQ) {
+                T::template multiply_columns<n - NS - DS>(dv, x[n % 2], py, [&](auto m_c) __attribute__((always_inline)) {
+                    share<8, 2 * KB * NQ, (n - NS - DS) * 2 * KB + decltype(m_c)::value>(slope);
+                });
+            } else T::template multiply_columns<n - NS - DS - NQ>(dk, x[n % 2], dsy, nothing);
+        });
+    };
+    auto some_of_tile = [&](int i0, const CYC_LDS char *here) __attribute__((always_inline)) {
+        const int p0 = i0 + shift, p1 = (i0 + TILE < N ? i0 + TILE : N) - 1 + shift;
+        if (kw >= M || p1 < kw || (kw >= sinks && (int64_t)p0 - kw_last >= window)) return;
+        const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
+        const int l = fresh(threadIdx.x & 63), g = l >> 4, lq = l & 15;
+        const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
+        static_for<DS / 2>([&](auto n_c) __attribute__((always_inline)) {
+            T::template request_rows<decltype(n_c)::value, 0>(x[0], row_at);
+            arrived<0, false>(x[0]);
+            T::template multiply_rows<decltype(n_c)::value>(s, x[0], kf, nothing);
+        });
+        static_for<DS>([&](auto n_c) __attribute__((always_inline)) {
+            request_values(n_c, x[0], row_at, v_at);
+            arrived<0, false>(x[0]);
+            multiply_values(n_c, x[0], nothing);
+        });
+        read_stats(lse, here + 2 * TILE_BYTES);
+        read_stats(Di, here + 2 * TILE_BYTES + 128);
+        auto visible = [&](int r, int n) __attribute__((always_inline)) {
+            const int position = p0 + r, key = kw + n * 16 + lq;
+            return (i0 + r < N) & (key <= position) & ((position - key < window) | (key < sinks));
+        };
+        static_for<16>([&](auto e_c) __attribute__((always_inline)) {
+            constexpr int e = decltype(e_c)::value, c = e / 8, n = e / 4 % 2, r = e % 4;
+            const bool seen = all | visible(c * 16 + 4 * g + r, n);
+            const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], scale, -lse[c][r])), dS = P * (dp[c][n][r] - Di[c][r]);
+            s[c][n][r] = seen ? P : 0.0f;
+            dp[c][n][r] = seen ? dS : 0.0f;
+        });
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) {
-                        const float P = __builtin_amdgcn_exp2f(__builtin_fmaf(s[n][r], scale, -lse[r]));
-                        s[n][r] = P;
-                        dp[n][r] = P * (dp[n][r] - Di[r]);
-                    }
-                if (!all) {
+        for (int n = 0; n < KB; ++n)
 #pragma unroll
-                    for (int n = 0; n < KB; ++n)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const bool seen = visible(c * 16 + 4 * g + r, n);
-                            s[n][r] = seen ? s[n][r] : 0.0f;
-                            dp[n][r] = seen ? dp[n][r] : 0.0f;
-                        }
-                }
-                pack<c>(py, s);
-                pack<c>(dsy, dp);
-            });
-            const bool careful = !all && (T::infinite(here, l) || T::infinite(here + TILE_BYTES, l));
-            if (CAREFUL && careful) {
-                T::accumulate_carefully(dv, column_address + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
-                T::accumulate_carefully(dk, column_address, here, l, dsy, visible, not_a_number);
-            } else {
-                marked |= careful;
-                T::template accumulate<TILE_BYTES>(dv, column_address, py);
-                T::template accumulate<0>(dk, column_address, dsy);
+            for (int i = 0; i < 4; ++i) {
+                py[n][i] = pack(s[i / 2][n][i % 2 * 2], s[i / 2][n][i % 2 * 2 + 1]);
+                dsy[n][i] = pack(dp[i / 2][n][i % 2 * 2], dp[i / 2][n][i % 2 * 2 + 1]);
             }
+        const bool careful = !all && (T::infinite(here, l) || T::infinite(here + TILE_BYTES, l));
+        if (CAREFUL && careful) {
+            T::accumulate_carefully(dv, column_at + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
+            T::accumulate_carefully(dk, column_at, here, l, dsy, visible, not_a_number);
+        } else {
+            marked |= careful;
+            T::template accumulate<TILE_BYTES>(dv, column_at, py);
+            T::template accumulate<0>(dk, column_at, dsy);
         }
-        const int turn = stage ? -STAGE : STAGE;
+    };
+    int u = u_first, i0 = 0;
+    auto arrive = [&]() __attribute__((always_inline)) {
+        landed_barrier();
+        i0 = next_tile * TILE;
+        advance(u);
+        if (u + 1 < u_last) issue(u + 1);
+    };
+    auto leave = [&]() __attribute__((always_inline)) {
+        const int turn = (u - u_first) & 1 ? -STAGE : STAGE;
         by_row += turn;
         by_column += turn;
+        ++u;
+    };
+    if (u_first < u_last) issue(u_first);
+    while (u < u_last && u < whole_tiles) {
+        arrive();
+        whole_tile(lds + ((u - u_first) & 1) * STAGE);
+        leave();
+    }
+    while (u < u_last) {
+        arrive();
+        some_of_tile(i0, lds + ((u - u_first) & 1) * STAGE);
+        leave();
     }
 
     if (!CAREFUL && l == 0) marks[mark + w] = marked;
