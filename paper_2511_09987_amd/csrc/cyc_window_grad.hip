@@ -300,12 +300,13 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
             if (k0 > p_hi || (k0 >= sinks && p_lo >= 0 && k1 < p_lo - window + 1)) continue;
             const bool all = k1 <= p_lo && (k0 >= p_hi - window + 1 || k1 < sinks);
             const uint32_t row_at = fresh(by_row) + half * TILE * ROW, column_at = fresh(by_column) + half * TILE * ROW;
+            T::template request_rows<0, 0>(x[0], row_at);
             static_for<DS>([&](auto n_c) __attribute__((always_inline)) {
                 constexpr int n = decltype(n_c)::value, j = n % (DS / 2);
-                T::template request_rows<j, n / (DS / 2) * 2 * TILE_BYTES>(x[0], row_at);
-                arrived<0, false>(x[0]);
-                if constexpr (n < DS / 2) T::template multiply_rows<j>(s[0], x[0], qf, nothing);
-                else T::template multiply_rows<j>(dp, x[0], of, nothing);
+                if constexpr (n + 1 < DS) T::template request_rows<(n + 1) % (DS / 2), (n + 1) / (DS / 2) * 2 * TILE_BYTES>(x[(n + 1) % 2], row_at);
+                arrived<(n + 1 < DS ? 4 : 0), false>(x[n % 2]);
+                if constexpr (n < DS / 2) T::template multiply_rows<j>(s[0], x[n % 2], qf, nothing);
+                else T::template multiply_rows<j>(dp, x[n % 2], of, nothing);
             });
             auto visible = [&](int key, int jq) __attribute__((always_inline)) { return (key <= row_hi[jq]) & ((key >= row_lo[jq]) | (key < sinks)); };
             static_for<16>([&](auto e_c) __attribute__((always_inline)) {
@@ -383,23 +384,24 @@ constexpr int KEYS = 64 * KEY_BLOCKS;
 // The code for tiles that are not all finite takes registers that the usual case does not have to spare (96 of them spilled, and
 // half the speed), so it has a launch of its own: CAREFUL false does without and leaves a mark where it met such a masked tile, CAREFUL true
 // does the marked workgroups again.
+
+// What a workgroup does, with its two stages and the values of its keys in `lds`.
+template <int D> constexpr int STAGE_BYTES = 2 * TILE * D * 2 + 1024;             // the tile of Q, that of dO, lse and D of its rows
+template <int D> constexpr int KEYS_LDS = 2 * STAGE_BYTES<D> + KEYS * D * 2;
 template <int D, bool CAREFUL>
-__global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
+__device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs &runs, float scale, const float *lse2, const float *Ds, float *part, int *marks, int block, CYC_LDS char *lds)
 {
     typedef Tile<D> T;
-    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB;
-    constexpr int TILE_BYTES = TILE * ROW, STAGE = 2 * TILE_BYTES + 1024;
-    // a stage: the tile of Q, that of dO, lse and D of its rows
-    __shared__ __attribute__((aligned(1024))) char lds_raw[2 * STAGE + KEYS * ROW];
-    CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
+    constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB, TILE_BYTES = TILE * ROW, STAGE = STAGE_BYTES<D>;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int mark = blockIdx.x * 4;
-    if (CAREFUL && marks[mark] + marks[mark + 1] + marks[mark + 2] + marks[mark + 3] == 0) return;
+    const int mark = block * 4;
     bool marked = false;
-    const Place at(blockIdx.x, p.batch * p.kv_heads, runs.per_pair());
-    const int pair = at.pair, slot = at.unit;
-    const int in_first = runs.first * runs.first_runs;
+    // the short runs of the first tiles before all others
+    const int pairs = p.batch * p.kv_heads, in_first = runs.first * runs.first_runs, sinks_end = pairs * in_first;
+    const bool early = block < sinks_end;
+    const Place at(early ? block : block - sinks_end, pairs, early ? in_first : runs.per_pair() - in_first);
+    const int pair = at.pair, slot = at.unit + (early ? 0 : in_first);
     const int tile = __builtin_amdgcn_readfirstlane(slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs);
     const int run = slot - runs.slot(tile), nruns = runs.runs_of(tile);
     const int64_t b = __builtin_amdgcn_readfirstlane(pair / p.kv_heads);
@@ -567,15 +569,19 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
         const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
         const int l = fresh(threadIdx.x & 63), g = l >> 4, lq = l & 15;
         const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
-        static_for<DS / 2>([&](auto n_c) __attribute__((always_inline)) {
-            T::template request_rows<decltype(n_c)::value, 0>(x[0], row_at);
-            arrived<0, false>(x[0]);
-            T::template multiply_rows<decltype(n_c)::value>(s, x[0], kf, nothing);
-        });
-        static_for<DS>([&](auto n_c) __attribute__((always_inline)) {
-            request_values(n_c, x[0], row_at, v_at);
-            arrived<0, false>(x[0]);
-            multiply_values(n_c, x[0], nothing);
+        constexpr int NS = DS / 2;
+        auto request = [&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            if constexpr (n < NS) T::template request_rows<n, 0>(x[n % 2], row_at);
+            else if constexpr (n < NS + DS) request_values(std::integral_constant<int, n - NS>{}, x[n % 2], row_at, v_at);
+        };
+        request(std::integral_constant<int, 0>{});
+        static_for<NS + DS>([&](auto n_c) __attribute__((always_inline)) {
+            constexpr int n = decltype(n_c)::value;
+            request(std::integral_constant<int, n + 1>{});
+            arrived<(n + 1 < NS + DS ? 4 : 0), false>(x[n % 2]);
+            if constexpr (n < NS) T::template multiply_rows<n>(s, x[n % 2], kf, nothing);
+            else multiply_values(std::integral_constant<int, n - NS>{}, x[n % 2], nothing);
         });
         read_stats(lse, here + 2 * TILE_BYTES);
         read_stats(Di, here + 2 * TILE_BYTES + 128);
@@ -663,6 +669,26 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     }
 }
 
+template <int D>
+__global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
+    keys_of_block<D, false>(p, runs, scale, lse2, Ds, part, marks, blockIdx.x, (CYC_LDS char *)lds);
+}
+// a few workgroups look through all marks
+template <int D>
+__global__ __launch_bounds__(256, 2) void grad_kv_careful_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
+{
+    __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
+    const int blocks = p.batch * p.kv_heads * runs.per_pair();
+    for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
+        const i32x4 m = ((const i32x4 *)marks)[block];
+        if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
+        keys_of_block<D, true>(p, runs, scale, lse2, Ds, part, marks, block, (CYC_LDS char *)lds);
+        landed_barrier();                                             // (LDS is free again)
+    }
+}
+
 // Adds the runs of a tile of keys in ascending order; a thread takes four d of a key's dK and dV.
 template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part)
 {
@@ -690,22 +716,45 @@ template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const W
     *(bf16x4 *)((char *)p.dV.base + b * p.dV.batch + head * p.dV.head + key * p.dV.row + c * 2) = v;
 }
 
-// The chip takes 512 workgroups at a time.  With fewer tiles of keys than that their rows are cut into runs of at least eight steps; the
-// tiles of sinks, which every later row sees, into runs as long as the other tiles' work.
+// How the rows of a tile of keys are cut.  The chip takes 512 workgroups at a time, which count in rounds: 496 and 64 of the same length last
+// twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so, 291 now).  The tiles of sinks, whose rows are all that
+// follow, go first in many short runs, which fill what the others leave over; those are cut where that makes fewer or shorter
+// rounds, at a cost: three steps of 32 rows to start a run, the partial sums, written and read, and a launch.
+constexpr int64_t MOST_PART = 128 << 20;
+
 Runs choose_runs(const WindowProblem &p)
 {
-    const int keys = KEYS;
-    Runs r = {(p.M + keys - 1) / keys, 0, 1, 1};
-    const int64_t pairs = (int64_t)p.batch * p.kv_heads;
-    const int64_t usual = std::min<int64_t>(p.N, (int64_t)p.window + keys), steps = (usual + TILE - 1) / TILE * p.group;
-    const int64_t all_steps = ((int64_t)p.N + TILE - 1) / TILE * p.group;
-    r.runs = (int)std::max<int64_t>(1, std::min({512 / std::max<int64_t>(1, pairs * r.tiles), steps / 8, (int64_t)64}));
-    r.first = (int)std::min<int64_t>(r.tiles, ((int64_t)std::min(p.sinks, p.M) + keys - 1) / keys);
-    if (p.window == INT_MAX) r.first = 0;
-    const int64_t run_steps = std::max<int64_t>(1, (steps + r.runs - 1) / r.runs);
-    r.first_runs = (int)std::max<int64_t>(r.runs, std::min<int64_t>((all_steps + run_steps - 1) / run_steps, 256));
-    if (r.first == 0) r.first_runs = r.runs;
-    return r;
+    Runs best = {(p.M + KEYS - 1) / KEYS, 0, 1, 1};
+    const int64_t pairs = (int64_t)p.batch * p.kv_heads, part = pairs * KEYS * p.d * 8;              // bytes of a run of a tile of each pair
+    const int64_t all_steps = ((int64_t)p.N + TILE - 1) / TILE * p.group, steps = std::min<int64_t>(all_steps, ((int64_t)p.window + KEYS + TILE - 1) / TILE * p.group);
+    const int64_t step = p.d == 128 ? 1500 : 900;                     // nanoseconds, two workgroups on a compute unit
+    const bool cut = steps < all_steps;                               // else every tile's rows are those that follow
+    int64_t early = 0, early_length = 0;                              // runs of sinks
+    if (cut && p.sinks > 0) {
+        best.first = (int)std::min<int64_t>(best.tiles, ((int64_t)std::min(p.sinks, p.M) + KEYS - 1) / KEYS);
+        best.first_runs = (int)std::max<int64_t>(1, std::min<int64_t>({(all_steps + 15) / 16, 1024 / (pairs * best.first), MOST_PART / 2 / (part * best.first)}));
+        early = pairs * best.first * best.first_runs;
+        early_length = all_steps / best.first_runs + 3;
+    }
+    const int64_t others = pairs * (best.tiles - best.first), mean = cut ? steps : (steps + 1) / 2;
+    int64_t best_cost = INT64_MAX;
+    for (int64_t r = 1; r == 1 || (r <= 32 && steps / r >= 8 && part * (best.tiles - best.first) * r <= MOST_PART / 2); ++r) {
+        const int64_t n = others * r, length = (mean + r - 1) / r + 3, longest = (steps + r - 1) / r + 3, work = (early * early_length + n * length) / 512;
+        int64_t time;                                                 // in steps
+        if (!cut) time = std::max(work, longest);                     // (rows of very different numbers even out)
+        else if (early + n <= 512) time = std::max(early_length, length);
+        else if (n <= 512) time = early_length + length;
+        else time = std::max(early_length + 2 * length, work + length / 2);
+        int64_t cost = time * step;
+        if (r > 1) cost += 6000 + part * (best.tiles - best.first) * r / 2000;
+        if (cost < best_cost) {
+            best_cost = cost;
+            best.runs = (int)r;
+        }
+    }
+    best.first_runs = std::max(best.first_runs, best.runs);
+    if (best.first == 0) best.first_runs = best.runs;
+    return best;
 }
 
 int64_t stats_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * padded_rows(p.N) * 8 + 255) / 256 * 256; }
@@ -724,11 +773,12 @@ template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace,
     hipError_t e = hipSuccess;
     if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs)), dim3(256), s, p, tiles, scale, lse2, Ds);
     if (e != hipSuccess || p.M == 0) return e;
-    auto keys_of = [&](auto kernel) {
-        return launch_kernel(kernel, dim3((unsigned)(runs.per_pair() * pairs)), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, marks);
+    const int64_t blocks = runs.per_pair() * pairs;
+    auto keys_of = [&](auto kernel, int64_t grid) {
+        return launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, marks);
     };
-    e = keys_of(grad_kv_kernel<D, false>);
-    if (e == hipSuccess) e = keys_of(grad_kv_kernel<D, true>);
+    e = keys_of(grad_kv_kernel<D>, blocks);
+    if (e == hipSuccess) e = keys_of(grad_kv_careful_kernel<D>, std::min<int64_t>(blocks, 256));
     if (e != hipSuccess || runs.kept_tiles() == 0) return e;
     const int64_t threads = pairs * runs.kept_tiles() * KEYS * (D / 4);
     return launch_kernel(grad_join_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), s, p, runs, (const float *)part);
