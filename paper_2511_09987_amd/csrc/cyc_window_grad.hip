@@ -389,7 +389,7 @@ constexpr int KEYS = 64 * KEY_BLOCKS;
 template <int D> constexpr int STAGE_BYTES = 2 * TILE * D * 2 + 1024;             // the tile of Q, that of dO, lse and D of its rows
 template <int D> constexpr int KEYS_LDS = 2 * STAGE_BYTES<D> + KEYS * D * 2;
 template <int D, bool CAREFUL>
-__device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs &runs, float scale, const float *lse2, const float *Ds, float *part, int *marks, int block, CYC_LDS char *lds)
+__device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs &runs, float scale, const float *lse2, const float *Ds, float *part, int *used, int *marks, int block, CYC_LDS char *lds)
 {
     typedef Tile<D> T;
     constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, KB = KEY_BLOCKS, KW = 16 * KB, TILE_BYTES = TILE * ROW, STAGE = STAGE_BYTES<D>;
@@ -563,9 +563,11 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
             } else T::template multiply_columns<n - NS - DS - NQ>(dk, x[n % 2], dsy, nothing);
         });
     };
+    bool touched = false;                                            // has this wave met a tile whose queries see any of its keys?
     auto some_of_tile = [&](int i0, const CYC_LDS char *here) __attribute__((always_inline)) {
         const int p0 = i0 + shift, p1 = (i0 + TILE < N ? i0 + TILE : N) - 1 + shift;
         if (kw >= M || p1 < kw || (kw >= sinks && (int64_t)p0 - kw_last >= window)) return;
+        touched = true;
         const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
         const int l = fresh(threadIdx.x & 63), g = l >> 4, lq = l & 15;
         const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
@@ -629,6 +631,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     if (u_first < u_last) issue(u_first);
     while (u < u_last && u < whole_tiles) {
         arrive();
+        touched = true;
         whole_tile(lds + ((u - u_first) & 1) * STAGE);
         leave();
     }
@@ -645,7 +648,11 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     for (int n = 0; n < KB; ++n) {
         const int key = kw + n * 16 + lq;
         if (nruns > 1) {
-            float *to = part + (((int64_t)pair * runs.kept_per_pair() + slot) * 2 * KEYS + w * KW + n * 16 + lq) * D;
+            // (most keys of a tile with sinks see nothing more after a while: nothing is kept of those)
+            const int64_t kept = (int64_t)pair * runs.kept_per_pair() + slot;
+            if (n == 0 && l == 0) used[kept * 4 + w] = touched;
+            if (!touched) continue;
+            float *to = part + (kept * 2 * KEYS + w * KW + n * 16 + lq) * D;
 #pragma unroll
             for (int id = 0; id < DT; ++id) {
                 *(f32x4 *)(to + id * 16 + 4 * g) = dk[id][n];
@@ -670,40 +677,57 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
 }
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
+__global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *used, int *marks)
 {
     __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
-    keys_of_block<D, false>(p, runs, scale, lse2, Ds, part, marks, blockIdx.x, (CYC_LDS char *)lds);
+    keys_of_block<D, false>(p, runs, scale, lse2, Ds, part, used, marks, blockIdx.x, (CYC_LDS char *)lds);
 }
 // a few workgroups look through all marks
 template <int D>
-__global__ __launch_bounds__(256, 2) void grad_kv_careful_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *marks)
+__global__ __launch_bounds__(256, 2) void grad_kv_careful_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *used, int *marks)
 {
     __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
     const int blocks = p.batch * p.kv_heads * runs.per_pair();
     for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
         const i32x4 m = ((const i32x4 *)marks)[block];
         if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
-        keys_of_block<D, true>(p, runs, scale, lse2, Ds, part, marks, block, (CYC_LDS char *)lds);
+        keys_of_block<D, true>(p, runs, scale, lse2, Ds, part, used, marks, block, (CYC_LDS char *)lds);
         landed_barrier();                                             // (LDS is free again)
     }
 }
 
-// Adds the runs of a tile of keys in ascending order; a thread takes four d of a key's dK and dV.
-template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part)
+// Adds the runs of a tile of keys in ascending order, those in which the keys' wave did anything; a thread takes four d of a key's dK and dV.
+constexpr int MOST_RUNS = 256;
+template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part, const int *used)
 {
-    const int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int c = (int)(x % (D / 4)) * 4, in_tile = (int)(x / (D / 4) % KEYS);
-    const int64_t rest = x / (D / 4) / KEYS;
-    const int tile = (int)(rest % runs.kept_tiles());
-    const int64_t pair = rest / runs.kept_tiles(), b = pair / p.kv_heads;
+    constexpr int PER = 1024 / D;                                     // keys of a workgroup, all of one wave of the other kernel
+    __shared__ int list[MOST_RUNS], counts[4];
+    const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int64_t block = blockIdx.x / (KEYS / PER);                   // (pair, tile)
+    const int in_tile = (int)(blockIdx.x % (KEYS / PER)) * PER + threadIdx.x / (D / 4), c = threadIdx.x % (D / 4) * 4;
+    const int tile = (int)(block % runs.kept_tiles()), n = runs.runs_of(tile);
+    const int64_t pair = block / runs.kept_tiles(), b = pair / p.kv_heads;
     const int head = (int)(pair % p.kv_heads), key = tile * KEYS + in_tile;
-    if (b >= p.batch || key >= p.M || runs.runs_of(tile) <= 1) return;
-    const float *from = part + ((pair * runs.kept_per_pair() + runs.slot(tile)) * 2 * KEYS + in_tile) * D + c;
+    const int64_t kept = pair * runs.kept_per_pair() + runs.slot(tile);
+    const bool mine = threadIdx.x < n && used[(kept + threadIdx.x) * 4 + in_tile / (16 * KEY_BLOCKS)];
+    const uint64_t votes = __builtin_amdgcn_ballot_w64(mine);
+    if (l == 0) counts[w] = __builtin_popcountll(votes);
+    __syncthreads();
+    int before = __builtin_popcountll(votes & (((uint64_t)1 << l) - 1)), count = 0;
+    for (int x = 0; x < 4; ++x) {
+        before += x < w ? counts[x] : 0;
+        count += counts[x];
+    }
+    if (mine) list[before] = threadIdx.x;
+    __syncthreads();
+    if (key >= p.M) return;
+    const float *from = part + (kept * 2 * KEYS + in_tile) * D + c;
     f32x4 dk = {0, 0, 0, 0}, dv = {0, 0, 0, 0};
-    for (int run = 0; run < runs.runs_of(tile); ++run, from += 2 * KEYS * D) {
-        dk += *(const f32x4 *)from;
-        dv += *(const f32x4 *)(from + KEYS * D);
+#pragma unroll 4
+    for (int x = 0; x < count; ++x) {
+        const float *run = from + (int64_t)list[x] * 2 * KEYS * D;
+        dk += *(const f32x4 *)run;
+        dv += *(const f32x4 *)(run + KEYS * D);
     }
     const float back = 1.0f / __builtin_sqrtf((float)D);
     bf16x4 u, v;
@@ -732,7 +756,7 @@ Runs choose_runs(const WindowProblem &p)
     int64_t early = 0, early_length = 0;                              // runs of sinks
     if (cut && p.sinks > 0) {
         best.first = (int)std::min<int64_t>(best.tiles, ((int64_t)std::min(p.sinks, p.M) + KEYS - 1) / KEYS);
-        best.first_runs = (int)std::max<int64_t>(1, std::min<int64_t>({(all_steps + 15) / 16, 1024 / (pairs * best.first), MOST_PART / 2 / (part * best.first)}));
+        best.first_runs = (int)std::max<int64_t>(1, std::min<int64_t>({(all_steps + 15) / 16, 1024 / (pairs * best.first), MOST_PART / 2 / (part * best.first), MOST_RUNS}));
         early = pairs * best.first * best.first_runs;
         early_length = all_steps / best.first_runs + 3;
     }
@@ -759,38 +783,45 @@ Runs choose_runs(const WindowProblem &p)
 
 int64_t stats_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * padded_rows(p.N) * 8 + 255) / 256 * 256; }
 
-int64_t marks_bytes(const WindowProblem &p) { return (int64_t)p.batch * p.kv_heads * choose_runs(p).per_pair() * 16; }
+// Where a call keeps what in its workspace, in bytes.
+struct Layout {
+    int64_t marks, used, part, end;
+    Layout(const WindowProblem &p, const Runs &runs)
+    {
+        const int64_t pairs = p.M > 0 ? (int64_t)p.batch * p.kv_heads : 0;
+        marks = stats_bytes(p);
+        used = marks + pairs * runs.per_pair() * 16;
+        part = used + pairs * runs.kept_per_pair() * 16;
+        end = part + pairs * runs.kept_per_pair() * 2 * KEYS * p.d * 4;
+    }
+};
 
 template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace, hipStream_t s)
 {
-    float *lse2 = (float *)workspace, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)((char *)workspace + stats_bytes(p) + (p.M > 0 ? marks_bytes(p) : 0));
-    int *marks = (int *)((char *)workspace + stats_bytes(p));
+    const Runs runs = choose_runs(p);
+    const Layout at(p, runs);
+    char *mem = (char *)workspace;
+    float *lse2 = (float *)mem, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)(mem + at.part);
+    int *marks = (int *)(mem + at.marks), *used = (int *)(mem + at.used);
     const float scale = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
     const int tiles = (int)(((int64_t)p.N * p.group + 127) / 128);
-    const int64_t pairs = (int64_t)p.batch * p.kv_heads;
-    const Runs runs = choose_runs(p);
-    if (tiles * pairs >= ((int64_t)1 << 31) || runs.per_pair() * pairs >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+    const int64_t pairs = (int64_t)p.batch * p.kv_heads, blocks = runs.per_pair() * pairs;
+    if (tiles * pairs >= ((int64_t)1 << 31) || blocks >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
     hipError_t e = hipSuccess;
     if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs)), dim3(256), s, p, tiles, scale, lse2, Ds);
     if (e != hipSuccess || p.M == 0) return e;
-    const int64_t blocks = runs.per_pair() * pairs;
     auto keys_of = [&](auto kernel, int64_t grid) {
-        return launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, marks);
+        return launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, used, marks);
     };
     e = keys_of(grad_kv_kernel<D>, blocks);
     if (e == hipSuccess) e = keys_of(grad_kv_careful_kernel<D>, std::min<int64_t>(blocks, 256));
     if (e != hipSuccess || runs.kept_tiles() == 0) return e;
-    const int64_t threads = pairs * runs.kept_tiles() * KEYS * (D / 4);
-    return launch_kernel(grad_join_kernel<D>, dim3((unsigned)((threads + 255) / 256)), dim3(256), s, p, runs, (const float *)part);
+    return launch_kernel(grad_join_kernel<D>, dim3((unsigned)(pairs * runs.kept_tiles() * (KEYS * D / 1024))), dim3(256), s, p, runs, (const float *)part, (const int *)used);
 }
 
 }  // namespace
 
-int64_t window_grad_workspace_bytes(const WindowProblem &p)
-{
-    const int64_t keys = KEYS;
-    return stats_bytes(p) + (p.M > 0 ? marks_bytes(p) + (int64_t)p.batch * p.kv_heads * choose_runs(p).kept_per_pair() * 2 * keys * p.d * 4 : 0);
-}
+int64_t window_grad_workspace_bytes(const WindowProblem &p) { return Layout(p, choose_runs(p)).end; }
 
 hipError_t launch_window_grad(const WindowProblem &p, void *workspace, int64_t, hipStream_t s)
 {
