@@ -5,7 +5,6 @@ fallback: if the shared library is missing, the first call raises ImportError.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 
@@ -481,23 +480,15 @@ def cyc_recurrence_attention_paged(Q: int, cache: cyc_cache, O: int, tokens: int
                                                      workspace_bytes, stream))
 
 
-@contextlib.contextmanager
-def _on(tensor, stream):
-    """The tensor's device as the current one, and `stream`, where one is given, as its current stream: what is allocated inside
-    comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it."""
+def _elsewhere(call, tensor, stream, *args):
+    """call(*args, stream) with the tensor's device as the current one and `stream`, where one is given, as its current stream: what is
+    allocated inside comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it."""
     import torch
     with torch.cuda.device(tensor.device):
         if isinstance(stream, torch.cuda.Stream) and stream.device == tensor.device:
             with torch.cuda.stream(stream):
-                yield
-        else:
-            yield
-
-
-def _place(tensor, stream):
-    """_on where it changes anything: entering it costs 3 us."""
-    import torch
-    return contextlib.nullcontext() if stream is None and tensor.device.index == torch.cuda.current_device() else _on(tensor, stream)
+                return call(*args, stream)
+        return call(*args, stream)
 
 
 def _mask_arguments(window, sinks):
@@ -509,37 +500,63 @@ def _mask_arguments(window, sinks):
     return window or 0, sinks
 
 
-def _check_rows(named, shape):
-    """bfloat16 device tensors of `shape` whose rows a kernel can read 16 bytes at a time."""
+def _device_of(name, t):
+    """The index of the device that a tensor lies on, which decides for the whole call."""
     import torch
-    for name, t in named:
-        if not t.is_cuda:
-            raise ValueError(f"{name} must be a device tensor; there is no CPU path")
-        if t.dtype != torch.bfloat16:
-            raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
-        if t.shape != shape:
-            raise ValueError(f"shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
-        if t.stride(-1) != 1 and t.numel() or t.data_ptr() & 15 or any(s % 8 for s in t.stride()[:-1]):
-            raise ValueError(f"{name} needs contiguous rows at multiples of 16 bytes")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor; there is no CPU path")
+    if t.dtype is not torch.bfloat16:
+        raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
+    return t.get_device()
 
 
-def _same_device(tensors):
-    device = tensors[0].device
-    if any(t.device != device for t in tensors):
+def _dense(t, shape, device, bfloat16) -> bool:
+    """The usual operand: all that _check_rows asks for, and contiguous."""
+    return t.is_cuda and t.dtype is bfloat16 and t.is_contiguous() and t.shape == shape and t.get_device() == device and not t.data_ptr() & 15
+
+
+def _check_rows(name, t, shape, device):
+    """A bfloat16 tensor of `shape` on `device` whose rows a kernel can read 16 bytes at a time."""
+    import torch
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor; there is no CPU path")
+    if t.dtype != torch.bfloat16:
+        raise ValueError(f"{name} must be bfloat16, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.get_device() != device:
         raise ValueError("all tensors must be on one device")
+    if t.stride(-1) != 1 and t.numel() or t.data_ptr() & 15 or any(s % 8 for s in t.stride()[:-1]):
+        raise ValueError(f"{name} needs contiguous rows at multiples of 16 bytes")
+
+
+def _operands(named, device):
+    """Strides of (name, tensor, shape) as the C ABI takes them, None where all are dense; raises where one will not do.  The
+    usual case is looked at first: a small call is over in 8 us, of which all checks one by one would be 4."""
+    import torch
+    bfloat16 = torch.bfloat16
+    if all([_dense(t, shape, device, bfloat16) for _, t, shape in named]):
+        return None
+    for name, t, shape in named:
+        _check_rows(name, t, shape, device)
+    return [s for _, t, _ in named for s in t.stride()[:-1]]
 
 
 def _attention_shapes(Q, K):
-    if Q.dim() != 4 or K.dim() != 4 or Q.shape[0] != K.shape[0] or Q.shape[3] != K.shape[3]:
-        raise ValueError(f"shape mismatch: Q {tuple(Q.shape)}, K {tuple(K.shape)}")
-    if Q.shape[3] not in (64, 128):
-        raise ValueError(f"the head dimension must be 64 or 128, got {Q.shape[3]}")
-    if K.shape[1] == 0 or Q.shape[1] % K.shape[1]:
-        raise ValueError(f"{Q.shape[1]} query heads do not divide among {K.shape[1]} key heads")
+    q, k = Q.shape, K.shape
+    if len(q) != 4 or len(k) != 4 or q[0] != k[0] or q[3] != k[3]:
+        raise ValueError(f"shape mismatch: Q {tuple(q)}, K {tuple(k)}")
+    if q[3] not in (64, 128):
+        raise ValueError(f"the head dimension must be 64 or 128, got {q[3]}")
+    if k[1] == 0 or q[1] % k[1]:
+        raise ValueError(f"{q[1]} query heads do not divide among {k[1]} key heads")
+    return q, k
 
 
-def _all_strides(tensors):
-    return None if all(t.is_contiguous() for t in tensors) else [s for t in tensors for s in t.stride()[:-1]]
+def _check_lse(lse, shape, device):
+    import torch
+    if not lse.is_cuda or lse.dtype != torch.float32 or lse.shape != shape or not lse.is_contiguous() or lse.get_device() != device:
+        raise ValueError("lse has the wrong shape, dtype, layout or device")
 
 
 def recurrence_attention_window(Q, K, V, window=None, sinks: int = 0, out=None, lse=None, stream=None):
@@ -548,33 +565,37 @@ def recurrence_attention_window(Q, K, V, window=None, sinks: int = 0, out=None, 
     Q: (batch, heads, N, d), K, V: (batch, kv_heads, M, d), torch.bfloat16 CUDA tensors with contiguous rows of d (64 or 128) and any
     strides otherwise that are multiples of 8 (so views of (batch, N, heads, d) will do); heads a multiple of kv_heads.  The
     queries are the last N of the M positions; position p sees the keys j <= p with p - j < window (None: all) or j < sinks.
-    Allocates O (bfloat16, like Q), lse (float32, (batch, heads, N): the logarithms of the sums, for the gradient) unless given, and
+    Allocates O (bfloat16, dense) and lse (float32, (batch, heads, N): the logarithms of the sums, for the gradient) unless given, and
     memory to split the keys of few queries over the chip, and forwards pointers to the C ABI on the current (or given) stream.
     (Where that memory is not to be had the keys are not split, and the fp32 sums are added in another order.)
     """
     import torch
-    _attention_shapes(Q, K)
-    _check_rows((("Q", Q),), Q.shape)
-    _check_rows((("K", K), ("V", V)), K.shape)
+    if Q.is_cuda and (stream is not None or Q.get_device() != torch.cuda.current_device()):
+        return _elsewhere(_attention_window, Q, stream, Q, K, V, window, sinks, out, lse)
+    return _attention_window(Q, K, V, window, sinks, out, lse, stream)
+
+
+def _attention_window(Q, K, V, window, sinks, out, lse, stream):
+    import torch
+    q, k = _attention_shapes(Q, K)
     window, sinks = _mask_arguments(window, sinks)
-    batch, heads, N, d = Q.shape
-    kv_heads, M = K.shape[1:3]
-    with _place(Q, stream):
-        if out is None:
-            out = torch.empty((batch, heads, N, d), dtype=torch.bfloat16, device=Q.device)
-        else:
-            _check_rows((("out", out),), Q.shape)
-        if lse is None:
-            lse = torch.empty((batch, heads, N), dtype=torch.float32, device=Q.device)
-        elif lse.shape != Q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
-            raise ValueError("lse has the wrong shape, dtype or layout")
-        _same_device((Q, K, V, out, lse))
-        s = _stream_handle(Q, stream)
+    batch, heads, N, d = q
+    kv_heads, M = k[1:3]
+    device = _device_of("Q", Q)
+    if out is None:
+        out = Q.new_empty(q)
+    strides = _operands((("Q", Q, q), ("K", K, k), ("V", V, k), ("out", out, q)), device)
+    if lse is None:
+        lse = Q.new_empty(q[:3], dtype=torch.float32)
+    else:
+        _check_lse(lse, q[:3], device)
+    s = _stream_handle(Q, stream)
+    work, wanted = None, 0
+    if M >= 512:                                  # the library splits no shorter list of keys
         wanted = cyc_attention_window_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
         work = _memory(wanted, Q, stream) if wanted else None
-        st = cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), batch, heads, kv_heads,
-                                             N, M, d, _all_strides((Q, K, V, out)), window, sinks, 0 if work is None else work.data_ptr(),
-                                             0 if work is None else wanted, s)
+    st = cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), batch, heads, kv_heads, N, M, d,
+                                         strides, window, sinks, 0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)
     if st != CYC_OK:
         raise CycError(st)
     return out, lse
@@ -583,55 +604,60 @@ def recurrence_attention_window(Q, K, V, window=None, sinks: int = 0, out=None, 
 def recurrence_attention_window_grad(Q, K, V, O, lse, dO, window=None, sinks: int = 0, dQ=None, dK=None, dV=None, stream=None):
     """Tensor-level convenience: (dQ, dK, dV) of recurrence_attention_window from what it returned and the gradient of O.
 
-    Q, K, V, window, sinks as in the forward call, O and lse what it returned, dO like O.  Allocates the gradients (bfloat16, like Q, K
-    and V) unless given and the memory that the call needs, and forwards pointers to the C ABI on the current (or given) stream.
+    Q, K, V, window, sinks as in the forward call, O and lse what it returned, dO like O.  Allocates the gradients (bfloat16, dense, of the
+    shapes of Q, K and V) unless given and the memory that the call needs, and forwards pointers to the C ABI on the current (or given)
+    stream.
     """
     import torch
-    _attention_shapes(Q, K)
-    _check_rows((("Q", Q), ("O", O), ("dO", dO)), Q.shape)
-    _check_rows((("K", K), ("V", V)), K.shape)
+    if Q.is_cuda and (stream is not None or Q.get_device() != torch.cuda.current_device()):
+        return _elsewhere(_attention_window_grad, Q, stream, Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV)
+    return _attention_window_grad(Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV, stream)
+
+
+def _attention_window_grad(Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV, stream):
+    q, k = _attention_shapes(Q, K)
     window, sinks = _mask_arguments(window, sinks)
-    batch, heads, N, d = Q.shape
-    kv_heads, M = K.shape[1:3]
-    if lse.shape != Q.shape[:3] or lse.dtype != torch.float32 or not lse.is_contiguous():
-        raise ValueError("lse has the wrong shape, dtype or layout")
-    with _place(Q, stream):
-        dQ = torch.empty(Q.shape, dtype=torch.bfloat16, device=Q.device) if dQ is None else dQ
-        dK = torch.empty(K.shape, dtype=torch.bfloat16, device=Q.device) if dK is None else dK
-        dV = torch.empty(K.shape, dtype=torch.bfloat16, device=Q.device) if dV is None else dV
-        _check_rows((("dQ", dQ),), Q.shape)
-        _check_rows((("dK", dK), ("dV", dV)), K.shape)
-        operands = (Q, K, V, O, dO, dQ, dK, dV)
-        _same_device((*operands, lse))
-        s = _stream_handle(Q, stream)
-        wanted = cyc_attention_window_grad_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
-        work = _memory(wanted, Q, stream) if wanted else None
-        st = cyc_recurrence_attention_window_grad(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(),
-                                                  dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), batch, heads, kv_heads, N, M, d,
-                                                  _all_strides(operands), window, sinks, 0 if work is None else work.data_ptr(),
-                                                  0 if work is None else wanted, s)
+    batch, heads, N, d = q
+    kv_heads, M = k[1:3]
+    device = _device_of("Q", Q)
+    dQ = Q.new_empty(q) if dQ is None else dQ
+    dK = Q.new_empty(k) if dK is None else dK
+    dV = Q.new_empty(k) if dV is None else dV
+    strides = _operands((("Q", Q, q), ("K", K, k), ("V", V, k), ("O", O, q), ("dO", dO, q), ("dQ", dQ, q), ("dK", dK, k), ("dV", dV, k)), device)
+    _check_lse(lse, q[:3], device)
+    s = _stream_handle(Q, stream)
+    wanted = cyc_attention_window_grad_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
+    work = _memory(wanted, Q, stream) if wanted else None
+    st = cyc_recurrence_attention_window_grad(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(), dQ.data_ptr(),
+                                              dK.data_ptr(), dV.data_ptr(), batch, heads, kv_heads, N, M, d, strides, window, sinks,
+                                              0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)
     if st != CYC_OK:
         raise CycError(st)
     return dQ, dK, dV
 
 
-def _cache(K_cache, V_cache, table, lengths, starts):
-    """The tensors of a cache, checked, as the C ABI takes them."""
+def _cache(K_cache, V_cache, table, lengths, starts, name, t):
+    """The tensors of a cache, checked, as the C ABI takes them, and the device of the call, that of tensor `t`."""
     import torch
-    if K_cache.dim() != 4 or K_cache.stride() != V_cache.stride():
+    shape, strides = K_cache.shape, K_cache.stride()
+    if len(shape) != 4 or strides != V_cache.stride():
         raise ValueError("K_cache and V_cache must be (pages, kv_heads, page, d) with the same strides")
-    _check_rows((("K_cache", K_cache), ("V_cache", V_cache)), K_cache.shape)
+    device = _device_of(name, t)
+    _operands((("K_cache", K_cache, shape), ("V_cache", V_cache, shape)), device)
+    int32 = torch.int32
     for name, t, dims in (("table", table, 2), ("lengths", lengths, 1), ("starts", starts, 1)):
-        if not t.is_cuda or t.dtype != torch.int32 or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        if not t.is_cuda or t.dtype is not int32 or t.dim() != dims or (not t.is_contiguous() and t.stride(-1) != 1):
             raise ValueError(f"{name} must be a device tensor of int32 with {dims} dimension(s) and contiguous rows")
-    pages, kv_heads, page, d = K_cache.shape
+        if t.get_device() != device:
+            raise ValueError("all tensors must be on one device")
+    pages, kv_heads, page, d = shape
     seqs, max_pages = table.shape
     if lengths.shape[0] != seqs or starts.shape[0] != seqs + 1:
         raise ValueError(f"{seqs} sequences need {seqs} lengths and {seqs + 1} starts, got {lengths.shape[0]} and {starts.shape[0]}")
     if page < 1 or page & (page - 1) or page > 65536 or d not in (64, 128):
         raise ValueError(f"pages hold a power of two of keys (up to 65536) of 64 or 128 elements, got {page} of {d}")
     return cyc_cache(K_cache.data_ptr(), V_cache.data_ptr(), table.data_ptr(), lengths.data_ptr(), starts.data_ptr(), seqs, pages, max_pages,
-                     kv_heads, page, d, table.stride(0), *K_cache.stride()[:3])
+                     kv_heads, page, d, table.stride(0), *strides[:3]), device
 
 
 def cache_append(K, V, K_cache, V_cache, table, lengths, starts, stream=None):
@@ -642,13 +668,17 @@ def cache_append(K, V, K_cache, V_cache, table, lengths, starts, stream=None):
     Rows starts[b] .. starts[b+1] - 1 of K and V become the last of the lengths[b] keys of sequence b; key j lies in row j % page of
     page table[b, j // page].  Tokens without a place (no sequence, key, or page) are not written.  Allocates nothing.
     """
-    import torch  # noqa: F401
-    cache = _cache(K_cache, V_cache, table, lengths, starts)
-    shape = (K.shape[0] if K.dim() else 0, K_cache.shape[1], K_cache.shape[3])
-    _check_rows((("K", K), ("V", V)), shape)
-    _same_device((K, V, K_cache, V_cache, table, lengths, starts))
-    with _place(K, stream):
-        st = cyc_cache_append(K.data_ptr(), V.data_ptr(), cache, shape[0], _all_strides((K, V)), _stream_handle(K, stream))
+    import torch
+    if K.is_cuda and K.get_device() != torch.cuda.current_device():
+        return _elsewhere(_append, K, stream, K, V, K_cache, V_cache, table, lengths, starts)
+    return _append(K, V, K_cache, V_cache, table, lengths, starts, stream)
+
+
+def _append(K, V, K_cache, V_cache, table, lengths, starts, stream):
+    cache, device = _cache(K_cache, V_cache, table, lengths, starts, "K", K)
+    shape = (K.shape[0] if K.dim() else 0, cache.kv_heads, cache.d)
+    strides = _operands((("K", K, shape), ("V", V, shape)), device)
+    st = cyc_cache_append(K.data_ptr(), V.data_ptr(), cache, shape[0], strides, _stream_handle(K, stream))
     if st != CYC_OK:
         raise CycError(st)
 
@@ -659,31 +689,36 @@ def recurrence_attention_paged(Q, K_cache, V_cache, table, lengths, starts, wind
     Q: (tokens, heads, d), torch.bfloat16; the cache, table, lengths and starts as in cache_append, heads a multiple of kv_heads; window
     and sinks as in recurrence_attention_window.  Rows starts[b] .. starts[b+1] - 1 of Q are the last positions of sequence b.  max_new: the
     most new tokens that any sequence brings, where the caller knows it: with 1, the usual step of a decoder, only the kernel for
-    few rows is launched (a sequence that brings more has NaN in its rows then).  Allocates O (bfloat16, like Q) unless given and memory to
+    few rows is launched (a sequence that brings more has NaN in its rows then).  Allocates O (bfloat16, dense) unless given and memory to
     split the keys over the chip, and forwards pointers to the C ABI on the current (or given) stream.
     """
     import torch
-    cache = _cache(K_cache, V_cache, table, lengths, starts)
-    if Q.dim() != 3 or Q.shape[2] != K_cache.shape[3]:
-        raise ValueError(f"shape mismatch: Q {tuple(Q.shape)}, K_cache {tuple(K_cache.shape)}")
-    _check_rows((("Q", Q),), Q.shape)
+    if Q.is_cuda and (stream is not None or Q.get_device() != torch.cuda.current_device()):
+        return _elsewhere(_attention_paged, Q, stream, Q, K_cache, V_cache, table, lengths, starts, window, sinks, max_new, out)
+    return _attention_paged(Q, K_cache, V_cache, table, lengths, starts, window, sinks, max_new, out, stream)
+
+
+def _attention_paged(Q, K_cache, V_cache, table, lengths, starts, window, sinks, max_new, out, stream):
+    cache, device = _cache(K_cache, V_cache, table, lengths, starts, "Q", Q)
+    q = Q.shape
+    if len(q) != 3 or q[2] != cache.d:
+        raise ValueError(f"shape mismatch: Q {tuple(q)}, K_cache {tuple(K_cache.shape)}")
     window, sinks = _mask_arguments(window, sinks)
     if max_new is not None and max_new < 1:
         raise ValueError(f"max_new must be at least 1, or None; got {max_new}")
-    tokens, heads, d = Q.shape
+    tokens, heads, _ = q
     if cache.kv_heads == 0 or heads % cache.kv_heads:
         raise ValueError(f"{heads} query heads do not divide among {cache.kv_heads} key heads")
-    with _place(Q, stream):
-        if out is None:
-            out = torch.empty((tokens, heads, d), dtype=torch.bfloat16, device=Q.device)
-        else:
-            _check_rows((("out", out),), Q.shape)
-        _same_device((Q, K_cache, V_cache, table, lengths, starts, out))
-        s = _stream_handle(Q, stream)
+    if out is None:
+        out = Q.new_empty(q)
+    strides = _operands((("Q", Q, q), ("out", out, q)), device)
+    s = _stream_handle(Q, stream)
+    work, wanted = None, 0
+    if cache.max_pages * cache.page >= 512:       # the library splits no shorter list of keys
         wanted = cyc_attention_paged_workspace(cache, tokens, heads, max_new or 0, window, sinks)
         work = _memory(wanted, Q, stream) if wanted else None
-        st = cyc_recurrence_attention_paged(Q.data_ptr(), cache, out.data_ptr(), tokens, heads, _all_strides((Q, out)), max_new or 0, window,
-                                            sinks, 0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)
+    st = cyc_recurrence_attention_paged(Q.data_ptr(), cache, out.data_ptr(), tokens, heads, strides, max_new or 0, window, sinks,
+                                        0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)
     if st != CYC_OK:
         raise CycError(st)
     return out
