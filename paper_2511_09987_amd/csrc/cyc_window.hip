@@ -37,38 +37,76 @@ struct TileProblem {
     // SHORT_ROWS for each (problem, key head)
     float *part, *refs;
     int64_t part_rows, rows;                                         // rows of a run there; rows of O
+    // paged, long sequences: splits is the most runs there may be, *chosen receives how many there are, none of more than most_tiles / runs tiles
+    int *chosen;
+    int most_tiles;
 };
 constexpr int LONG_ROWS = 128, SHORT_ROWS = 16;
+constexpr int LEAST_TILES = 8;           // of a run of few rows: what pays for its start
 
 enum Addressing { DENSE, PAGED_SHORT, PAGED_LONG };
 
-// Which sequence the slot-th tile of `per` rows belongs to and which of its tiles it is, counting the tiles of all sequences with more than
-// `less` rows one after the other: 64 sequences at a time, a lane counts for one.  False behind the last.
-__device__ __forceinline__ bool sequence_of_slot(const int *starts, int seqs, int tokens, int group, int per, int less, int slot, int *seq, int *tile)
+// What a workgroup finds out about the sequences of its call, 64 at a time, a lane for each.
+__device__ __forceinline__ int wave_most(int x)
 {
-    const int l = threadIdx.x & 63;
-    for (int b0 = 0; b0 < seqs; b0 += 64) {
-        const int b = b0 + l;
-        int first = b < seqs ? starts[b] : 0, end = b < seqs ? starts[b + 1] : 0;
-        first = first < 0 ? 0 : first > tokens ? tokens : first;
-        end = end < first ? first : end > tokens ? tokens : end;
-        const int rows = (end - first) * group, tiles = rows > less ? (rows + per - 1) / per : 0;
-        int upto = tiles;                                  // of the sequences b0 .. b
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int below = __shfl_up(upto, d);
-            upto += l >= d ? below : 0;
-        }
-        const uint64_t past = __builtin_amdgcn_ballot_w64(upto > slot);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            *seq = b0 + at;
-            *tile = slot - __builtin_amdgcn_readlane(upto - tiles, at);
-            return true;
-        }
-        slot -= __builtin_amdgcn_readlane(upto, 63);
+    for (int d = 32; d; d >>= 1) {
+        const int y = __shfl_xor(x, d);
+        x = x > y ? x : y;
     }
-    return false;
+    return __builtin_amdgcn_readfirstlane(x);
+}
+// the most keys of any
+__device__ __forceinline__ int most_keys(const int *lengths, int seqs)
+{
+    int most = 0;
+    for (int b = threadIdx.x & 63; b < seqs; b += 64) most = lengths[b] > most ? lengths[b] : most;
+    return wave_most(most);
+}
+// The tiles of `per` rows of the sequences with more than `less` rows, one sequence after the other: how many there are, the most keys of such a
+// sequence and, for one tile, which sequence it belongs to and which of its tiles it is.
+struct Tiles {
+    int total = 0, keys = 0, seq = -1, tile = 0;
+    // all: look at all sequences (total and keys are right then), not only up to the tile's
+    __device__ __forceinline__ void find(const TileProblem &p, int per, int slot, bool all)
+    {
+        const int l = threadIdx.x & 63;
+        int most = 0;
+        for (int b0 = 0; b0 < p.batch && (all || seq < 0); b0 += 64) {
+            const int b = b0 + l;
+            int first = b < p.batch ? p.starts[b] : 0, end = b < p.batch ? p.starts[b + 1] : 0;
+            const int length = all && b < p.batch ? p.lengths[b] : 0;
+            first = first < 0 ? 0 : first > p.tokens ? p.tokens : first;
+            end = end < first ? first : end > p.tokens ? p.tokens : end;
+            const int rows = (end - first) * p.group, tiles = rows > p.short_rows ? (rows + per - 1) / per : 0;
+            most = tiles > 0 && length > most ? length : most;
+            int upto = tiles;                              // of the sequences b0 .. b
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) {
+                const int below = __shfl_up(upto, d);
+                upto += l >= d ? below : 0;
+            }
+            const uint64_t past = __builtin_amdgcn_ballot_w64(total + upto > slot);
+            if (past && seq < 0) {
+                const int at = __builtin_ctzll(past);
+                seq = b0 + at;
+                tile = slot - total - __builtin_amdgcn_readlane(upto - tiles, at);
+            }
+            total += __builtin_amdgcn_readlane(upto, 63);
+        }
+        if (all) keys = wave_most(most);
+    }
+};
+
+// Many rows: the time in nanoseconds of `groups` workgroups, each walking up to `tiles` tiles of keys, that are cut into `runs` runs each.  The chip
+// holds 512, two on a compute unit, which take 1900 ns a tile of 64 keys x 128 rows x d 128 together (128 keys x d 64: 3100, twice the
+// weights), or 1650 (2600) where there is one; to start takes 4 us.  Runs add a launch and the partial outputs, which are written and read
+// at 3 TB/s.  (1024 + 7 x 1 tokens behind 6800 keys, 8 key heads, 256 workgroups: one run 215 us, three 158, two 120.)
+__host__ __device__ inline int64_t long_cost(int64_t groups, int64_t tiles, int64_t runs, int64_t rows, int64_t d)
+{
+    const int64_t all = groups * runs, full = all / 512, rest = all % 512, length = (tiles + runs - 1) / runs;
+    const int64_t two = (d == 128 ? 1900 : 3100) * length + 4000, one = (d == 128 ? 1650 : 2600) * length + 4000;
+    return full * two + (rest == 0 ? 0 : rest <= 256 ? one : two) + (runs > 1 ? 6000 + rows * (d + 2) * 4 * runs / 3000 : 0);
 }
 
 // D: head dimension; KT: keys per tile; NWAVE waves of QB * 16 rows.
@@ -92,7 +130,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4;
     const int w = NWAVE == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int splits = p.splits;
+    int splits = p.splits, run_tiles = p.run_tiles;       // runs of keys and tiles in each
     int b, head, tile, run, N = p.N, M = p.M, first = 0; // problem, key head, tile of rows, run of keys; queries, keys, first token
     bool bad = false;
     if constexpr (A == DENSE) {
@@ -112,12 +150,39 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             b = pair / p.kv_heads;
             head = pair - b * p.kv_heads;
             tile = 0;
+            // the host knows how wide the table is, not how long the sequences are: runs as long as the longest one needs
+            if (splits > 1) {
+                const int most = (most_keys(p.lengths, p.batch) + KT - 1) / KT, length = (most + splits - 1) / splits;
+                run_tiles = length < LEAST_TILES ? LEAST_TILES : length < run_tiles ? length : run_tiles;
+            }
         } else {
-            const Place at(blockIdx.x, p.kv_heads, p.tiles * splits);
-            const int slot = at.unit / splits;
-            run = at.unit - slot * splits;
-            head = at.pair;
-            if (!sequence_of_slot(p.starts, p.batch, p.tokens, p.group, ROWS, p.short_rows, slot, &b, &tile)) return;
+            // Likewise, and how many runs is decided here too, where the number of tiles of rows is known.  All workgroups that have work come
+            // first: 504 of them fill the chip's 512 places as long as none is held by one that only finds nothing to do.
+            Tiles rows;
+            int work = blockIdx.x / p.kv_heads;
+            if (splits > 1) {
+                rows.find(p, ROWS, -1, true);
+                const int most = (rows.keys + KT - 1) / KT, tiles = most < p.most_tiles ? most : p.most_tiles;
+                int64_t best = long_cost((int64_t)rows.total * p.kv_heads, tiles, 1, p.rows, D);
+                int runs = 1;
+                for (int r = 2; r <= splits && r * 4 <= tiles; ++r) {
+                    const int64_t cost = long_cost((int64_t)rows.total * p.kv_heads, tiles, r, p.rows, D);
+                    runs = cost < best ? r : runs;
+                    best = cost < best ? cost : best;
+                }
+                splits = __builtin_amdgcn_readfirstlane(runs);
+                run_tiles = __builtin_amdgcn_readfirstlane((tiles + runs - 1) / runs);
+                if (blockIdx.x == 0 && threadIdx.x == 0) *p.chosen = splits;
+            }
+            // (eight neighbours, whose key heads are different or whose tiles follow one another, run on the eight XCDs)
+            head = blockIdx.x - work * p.kv_heads;
+            const int slot = work / splits;
+            run = work - slot * splits;
+            rows = Tiles();
+            rows.find(p, ROWS, slot, false);
+            if (rows.seq < 0) return;
+            b = rows.seq;
+            tile = rows.tile;
         }
         int start = p.starts[b], end = p.starts[b + 1];
         M = p.lengths[b];
@@ -152,8 +217,8 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     // ---- the keys that the rows of the workgroup see, and this run's share of their tiles (none, if the list ends before)
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
     const KeyList<KT> list(row_first, row_last, group, N, M, window, sinks);
-    const int u_first = run * p.run_tiles, left = list.count - u_first;
-    const int ntiles = left < p.run_tiles || run == splits - 1 ? left : p.run_tiles;
+    const int u_first = run * run_tiles, left = list.count - u_first;
+    const int ntiles = left < run_tiles || run == splits - 1 ? left : run_tiles;
     auto tile_key = [&](int u) __attribute__((always_inline)) { return list.tile_key(u + u_first); };
 
     // ---- this wave's rows: first and last position, and per lane what its rows (one per 16-row block) see
@@ -420,7 +485,7 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
 #pragma unroll
                         for (int jq = 0; jq < QB; ++jq)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) acc_o[id][jq][r] += visible(key0 + key, jq) & !__builtin_isfinite((float)v[r]) ? (float)v[r] : 0.0f;
+                            for (int r = 0; r < 4; ++r) acc_o[id][jq][r] += (visible(key0 + key, jq) & !__builtin_isfinite((float)v[r])) ? (float)v[r] : 0.0f;
                     }
                 }
             }
@@ -537,7 +602,8 @@ template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(
         few = shorts.splits > 0;
         if (few) at = (b * p.kv_heads + h / p.group) * SHORT_ROWS + i * p.group + h % p.group;
     }
-    const Parts from = few ? shorts : longs;
+    Parts from = few ? shorts : longs;
+    if (PAGED && !few && from.splits > 1) from.splits = *p.chosen;
     if (from.splits <= 1) return;
     const float *ref = from.refs + at * 2, *part = from.part + at * D + c;
     float m = -__builtin_inff();
@@ -583,7 +649,12 @@ struct Mapping {
 };
 
 int64_t part_bytes(int64_t rows, int64_t d, int splits) { return splits > 1 ? (rows * splits * (d + 2) * 4 + 15) / 16 * 16 : 0; }
-int64_t workspace_bytes_of(const Mapping &m, int64_t d) { return part_bytes(m.short_rows, d, m.shorts.count) + part_bytes(m.long_rows, d, m.longs.count); }
+// (and 16 bytes for what the device chooses)
+int64_t workspace_bytes_of(const Mapping &m, int64_t d)
+{
+    const int64_t parts = part_bytes(m.short_rows, d, m.shorts.count) + part_bytes(m.long_rows, d, m.longs.count);
+    return parts > 0 ? parts + 16 : 0;
+}
 constexpr int64_t MOST_PART = 128 << 20;
 
 // Few rows: memory is the bound.  Keys of equal lists stream best through two workgroups on a compute unit (16 x 8 key heads x 8192 keys of
@@ -592,29 +663,26 @@ constexpr int64_t MOST_PART = 128 << 20;
 // 247).  A run has at least eight tiles, which pays for its start.
 Runs choose_short(int64_t pairs, int64_t tiles, int64_t rows, int64_t d, int64_t groups)
 {
-    return runs_of(tiles, std::max<int64_t>(std::min<int64_t>({MOST_PART / (rows * (d + 2) * 4), tiles / 8, groups / pairs, 64}), 1));
+    return runs_of(tiles, std::max<int64_t>(std::min<int64_t>({MOST_PART / (rows * (d + 2) * 4), tiles / LEAST_TILES, groups / pairs, 64}), 1));
 }
 
-// Many rows: by a cost in nanoseconds.  The chip holds 512 of these workgroups, two on a compute unit, which take 1900 ns a tile of 64 keys x 128
-// rows x d 128 together, or 1050 where there is one; how many there are is an estimate for sequences in pages, so that a last round
-// counts a quarter more than what it holds and not for a whole one.  A run adds 4 us of start and, all together, a launch and the
-// partial outputs, read at 3 TB/s.
+// Many rows: the runs that long_cost says, of `most` at most.
+constexpr int MOST_RUNS = 16;
 Runs choose_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
 {
-    Runs best;
-    int64_t best_cost = INT64_MAX;
-    for (int64_t want = 1; want == 1 || (want * 4 <= tiles && want <= 16); ++want) {
-        const Runs r = runs_of(tiles, want);
-        const int64_t part = part_bytes(rows, d, r.count), all = groups * r.count;
-        if (part > MOST_PART) break;
-        int64_t cost = all <= 256 ? 1050 * r.length + 4000 : (1900 * r.length + 4000) * std::max<int64_t>(512, all + 128) / 512;
-        if (r.count > 1) cost += 5000 + part / 3000;
-        if (cost < best_cost) {
-            best_cost = cost;
-            best = r;
-        }
-    }
-    return best;
+    int64_t best = 1;
+    for (int64_t r = 2; r <= MOST_RUNS && r * 4 <= tiles && rows * (d + 2) * 4 * r <= MOST_PART; ++r)
+        if (long_cost(groups, tiles, r, rows, d) < long_cost(groups, tiles, best, rows, d)) best = r;
+    return runs_of(tiles, best);
+}
+// Sequences in pages: the device decides (tile_kernel) and needs a grid and memory for what it may choose.  Runs come into question below four
+// rounds of workgroups, and where one run leaves no compute unit free only for lists that pay for it: to count the sequences takes each workgroup
+// more than 1 us, and a chip full of workgroups with 19 tiles each takes 60 us without and 65 with.
+Runs most_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
+{
+    if (groups > 256 && tiles < 32) return {1, (int)tiles};
+    const int64_t most = std::min<int64_t>({MOST_RUNS / 2, tiles / 4, MOST_PART / (rows * (d + 2) * 4), 2048 / std::max<int64_t>(groups, 1)});
+    return {(int)std::max<int64_t>(most, 1), (int)tiles};
 }
 
 // Tiles of kt keys that a workgroup's rows, `rows` of them at `queries` positions or fewer, see at most among `keys`.
@@ -644,12 +712,8 @@ Mapping paged_mapping(const PagedProblem &p)
     m.short_rows = (int64_t)p.seqs * p.kv_heads * SHORT_ROWS;
     m.long_rows = rows;
     const bool longs = (int64_t)p.max_new * p.group > SHORT_ROWS;
-    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), m.short_rows, p.d, 3072);
-    if (longs) {
-        // sequences with many rows: at most as many as what the longest leaves would make; each has half a tile that is not full
-        const int64_t most = std::min<int64_t>(p.seqs, 1 + (p.tokens - p.max_new) / (SHORT_ROWS / p.group + 1));
-        m.longs = choose_long(((int64_t)p.tokens * p.group / LONG_ROWS + most / 2) * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
-    }
+    if (!longs || (p.seqs > 1 && p.group <= SHORT_ROWS)) m.shorts = choose_short((int64_t)p.seqs * p.kv_heads, tiles(SHORT_ROWS, 4096 / p.d), m.short_rows, p.d, 3200);
+    if (longs) m.longs = most_long((int64_t)p.tokens * p.group / LONG_ROWS * p.kv_heads, tiles(LONG_ROWS, 8192 / p.d), rows, p.d);
     return m;
 }
 
@@ -657,7 +721,9 @@ template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, Mapping m, v
 {
     if (workspace_bytes_of(m, D) > workspace_bytes)
         for (Runs *r : {&m.shorts, &m.longs})
-            if (r->count) *r = {1, r->count * r->length};
+            if (r->count) *r = {1, INT_MAX};
+    t.chosen = (int *)((char *)workspace + workspace_bytes_of(m, D) - 16);
+    t.most_tiles = m.longs.length;
     t.scale_log2e = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
     char *free = (char *)workspace;
     auto launch = [&](auto kernel, int threads, int64_t groups, const Runs &runs, int64_t rows, Parts *parts) {

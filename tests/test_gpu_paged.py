@@ -111,6 +111,26 @@ def test_pages_that_a_window_has_passed(lib, window, sinks):
     batch.check(lib.recurrence_attention_paged(batch.Q, *batch.arguments(), window=window, sinks=sinks), window, sinks)
 
 
+@pytest.mark.parametrize("new,lengths", [([1, 1, 1], [700, 40, 1300]), ([1, 150, 3, 1], [2000, 1500, 64, 300]), ([260], [3000])])
+@pytest.mark.parametrize("workspace", (True, False))
+def test_a_table_far_wider_than_its_sequences(lib, new, lengths, workspace):
+    """How the keys are split goes by the lengths on the device, not by what the table could hold; and without memory they are not."""
+    batch = Batch(new, lengths, 8, 2, 128, 16, 13)
+    table = torch.full((len(new), 8192), -1, dtype=torch.int32, device=DEV)
+    table[:, :batch.table.shape[1]] = batch.table
+    O = torch.empty_like(batch.Q)
+    cache = lib.cyc_cache(batch.caches[0].data_ptr(), batch.caches[1].data_ptr(), table.data_ptr(), batch.lens.data_ptr(), batch.starts.data_ptr(),
+                          len(new), batch.caches[0].shape[0], 8192, 2, 16, 128, 8192, *batch.caches[0].stride()[:3])
+    wanted = lib.cyc_attention_paged_workspace(cache, batch.rows[-1], 8, 0, 0, 0)
+    assert wanted > 0
+    work = torch.full((wanted + 64,), 255, dtype=torch.uint8, device=DEV)
+    for size in (wanted, wanted - 1) if workspace else (0,):
+        assert lib.cyc_recurrence_attention_paged(batch.Q.data_ptr(), cache, O.data_ptr(), batch.rows[-1], 8, None, 0, 0, 0,
+                                                  work.data_ptr() if size else 0, size, torch.cuda.current_stream().cuda_stream) == 0
+        batch.check(O, None, 0)
+    assert bool((work[wanted:] == 255).all())
+
+
 def test_rows_that_belong_to_nobody(lib):
     batch = Batch([3, 0, 20], [70, 5, 300], 4, 2, 64, 16, 5)
     Q = torch.cat([batch.Q, normal((9, 4, 64), 1)])
