@@ -318,6 +318,7 @@ int cyc_recurrence_attention_window(const void *Q, const void *K, const void *V,
  * that see nothing and keys that nobody sees get zeros.  No atomic adds: the same call gives the same bits every time.
  * workspace: device, 16-byte aligned, not cleared, free again when the call's work on `stream` is done; the call needs
  * cyc_attention_window_grad_workspace bytes and returns CYC_ERR_WORKSPACE with nothing enqueued if it gets less.
+ * heads 0, or N 0: zeros for the keys.  batch or kv_heads 0, or N and M 0: CYC_OK, nothing done.
  * Extents and errors otherwise: those of the forward call, kv_heads * M below 2^30; none of dQ, dK, dV may meet itself or overlap another operand. */
 int64_t cyc_attention_window_grad_workspace(int64_t batch, int64_t heads, int64_t kv_heads, int64_t N, int64_t M, int64_t d,
                                             int64_t window, int64_t sinks);
@@ -345,7 +346,7 @@ typedef struct {
  * max_pages, or whose page is not in [0, pages), is not written; starts outside [0, tokens] leave their sequence unwritten.  Two tokens
  * of one call that the table sends to the same place leave either.
  * tokens or seqs == 0: CYC_OK, nothing done.  Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE, CYC_ERR_ALIAS (the cache
- * overlaps K, V, table, lengths or starts, or keeps keys and values in the same place), CYC_ERR_LAUNCH. */
+ * overlaps K, V, table, lengths or starts, or its keys and values have memory in common), CYC_ERR_LAUNCH. */
 int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64_t tokens, const int64_t *strides, void *stream);
 
 /* Attention of new tokens, one or many to a sequence, over the cache that holds them already: the mask and arithmetic of

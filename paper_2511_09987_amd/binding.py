@@ -591,7 +591,7 @@ def _attention_window(Q, K, V, window, sinks, out, lse, stream):
         _check_lse(lse, q[:3], device)
     s = _stream_handle(Q, stream)
     work, wanted = None, 0
-    if M >= 512:                                  # the library splits no shorter list of keys
+    if M >= 512:                                  # shorter lists of keys are not worth splitting
         wanted = cyc_attention_window_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
         work = _memory(wanted, Q, stream) if wanted else None
     st = cyc_recurrence_attention_window(Q.data_ptr(), K.data_ptr(), V.data_ptr(), out.data_ptr(), lse.data_ptr(), batch, heads, kv_heads, N, M, d,
@@ -714,7 +714,7 @@ def _attention_paged(Q, K_cache, V_cache, table, lengths, starts, window, sinks,
     strides = _operands((("Q", Q, q), ("out", out, q)), device)
     s = _stream_handle(Q, stream)
     work, wanted = None, 0
-    if cache.max_pages * cache.page >= 512:       # the library splits no shorter list of keys
+    if cache.max_pages * cache.page >= 512:       # shorter lists of keys are not worth splitting
         wanted = cyc_attention_paged_workspace(cache, tokens, heads, max_new or 0, window, sinks)
         work = _memory(wanted, Q, stream) if wanted else None
     st = cyc_recurrence_attention_paged(Q.data_ptr(), cache, out.data_ptr(), tokens, heads, strides, max_new or 0, window, sinks,

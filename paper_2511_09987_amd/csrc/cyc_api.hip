@@ -9,6 +9,8 @@
 #include <atomic>
 #include <algorithm>
 #include <climits>
+#include <cstdlib>
+#include <utility>
 
 namespace {
 
@@ -377,6 +379,22 @@ bool cache_extents(const cyc_cache &c, int64_t tokens, int *shift)
     if (!mul_ok(c.max_pages, c.page, &t) || t >= (1 << 30) || tokens >= (1 << 30) || !mul_ok(c.seqs, c.table_stride, &t)) return false;
     return strides_ok({nullptr, {c.pages, c.kv_heads, c.page}, {c.page_stride, c.head_stride, c.row_stride}, true}, c.d);
 }
+// Do keys and values share memory, other than by lying between one another?  Strides nest (strides_ok), so that of the steps of one extent
+// only the two next to what is left can bring two rows within d of each other, the largest stride first.
+bool caches_meet(const cyc_cache &c)
+{
+    const int64_t between = ((intptr_t)c.V - (intptr_t)c.K) / 2;
+    std::pair<int64_t, int64_t> steps[3] = {{c.page_stride, c.pages}, {c.head_stride, c.kv_heads}, {c.row_stride, c.page}};
+    std::sort(steps, steps + 3, [](auto &a, auto &b) { return a.first > b.first; });
+    auto meet = [&](auto &self, int64_t left, int i) -> bool {
+        if (i == 3) return std::abs(left) < c.d;
+        const auto [stride, extent] = steps[i];
+        if (extent == 1) return self(self, left, i + 1);
+        const int64_t n = left / stride - (left % stride < 0);
+        return (std::abs(n) < extent && self(self, left - n * stride, i + 1)) || (std::abs(n + 1) < extent && self(self, left - (n + 1) * stride, i + 1));
+    };
+    return meet(meet, between, 0);
+}
 int64_t cache_span(const cyc_cache &c) { return span_of({nullptr, {c.pages, c.kv_heads, c.page}, {c.page_stride, c.head_stride, c.row_stride}, true}, c.d); }
 
 bool overlaps_indices(const cyc_cache &c, const void *p, int64_t bytes)
@@ -591,7 +609,8 @@ int64_t cyc_attention_window_grad_workspace(int64_t batch, int64_t heads, int64_
                                             int64_t window, int64_t sinks)
 {
     cyc::WindowProblem p;
-    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || batch == 0 || heads == 0 || kv_heads * M >= (1 << 30)) return 0;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || batch == 0 || kv_heads == 0 || kv_heads * M >= (1 << 30)) return 0;
+    if (heads == 0) p.N = 0;
     return cyc::window_grad_workspace_bytes(p);
 }
 
@@ -601,8 +620,9 @@ int cyc_recurrence_attention_window_grad(const void *Q, const void *K, const voi
                                          int64_t workspace_bytes, void *stream)
 {
     cyc::WindowProblem p;
-    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || kv_heads * M >= (1 << 30)) return CYC_ERR_SHAPE;
-    if (batch == 0 || heads == 0 || (N == 0 && M == 0)) return CYC_OK;
+    if (!window_extents(batch, heads, kv_heads, N, M, d, window, sinks, &p) || (batch > 0 && kv_heads * M >= (1 << 30))) return CYC_ERR_SHAPE;
+    if (heads == 0) N = p.N = 0;                  // nobody reads the keys: zeros for them
+    if (batch == 0 || kv_heads == 0 || (N == 0 && M == 0)) return CYC_OK;
     if (!workspace || workspace_bytes < 0) workspace_bytes = 0;
     Operand x[8];
     const Named named[8] = {{Q, false, false}, {K, true, false}, {V, true, false}, {O, false, false},
@@ -631,7 +651,7 @@ int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64
     if (((uintptr_t)K | (uintptr_t)V | (uintptr_t)c.K | (uintptr_t)c.V) & 15 || ((uintptr_t)c.table | (uintptr_t)c.lengths | (uintptr_t)c.starts) & 3)
         return CYC_ERR_SHAPE;
     const int64_t span = cache_span(c);
-    if (c.K == c.V) return CYC_ERR_ALIAS;
+    if (caches_meet(c)) return CYC_ERR_ALIAS;
     for (const void *pool : {c.K, c.V}) {
         for (const Operand &o : x)
             if (overlaps(pool, span, o.p, span_of(o, c.d))) return CYC_ERR_ALIAS;

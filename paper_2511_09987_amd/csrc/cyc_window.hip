@@ -9,7 +9,7 @@
 // O^T = V^T P^T).  A wave skips the tiles that none of its rows sees and masks only those that some row sees in part.
 // Rows see different keys, so what must not reach a row is kept out twice: a masked score becomes -inf, its weight 0; and since 0 times
 // an infinity or NaN in V would still spoil the sum, a masked tile whose values are not all finite is multiplied without those,
-// which then go to the rows that see them (careful_values).  Keys that no row of the workgroup sees are not read at all: rows
+// which then go to the rows that see them.  Keys that no row of the workgroup sees are not read at all: rows
 // of a tile outside [0, sinks) and the window's span are copied from a key inside.
 #include "cyc_window.h"
 #include "cyc_tile.h"

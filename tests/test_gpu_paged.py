@@ -321,3 +321,20 @@ def test_two_streams_at_once(lib):
         b.check(out[0], None, 0)
         for o in out[1:]:
             assert torch.equal(o.view(torch.int16), out[0].view(torch.int16))
+
+
+@pytest.mark.parametrize("dim", (1, 3, 4))
+def test_append_to_keys_and_values_in_one_pool(lib, dim):
+    """Keys and values page by page, row by row, and halves of a row: they lie between one another and are written as if apart."""
+    shape = [6, 2, 16, 64]
+    pool = torch.zeros(shape[:dim] + [2] + shape[dim:], dtype=torch.bfloat16, device=DEV) if dim < 4 else \
+        torch.zeros(shape[:3] + [128], dtype=torch.bfloat16, device=DEV)
+    K_cache, V_cache = pool.unbind(dim) if dim < 4 else pool.split(64, -1)
+    g = torch.Generator(device=DEV).manual_seed(dim)
+    K, V = (torch.empty((9, 2, 64), dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    number = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    lib.cache_append(K, V, K_cache, V_cache, number(3, 1).view(1, 2), number(20), number(0, 9))
+    for cache, rows in ((K_cache, K), (V_cache, V)):
+        flat = torch.cat([cache[3], cache[1]], 1).transpose(0, 1)             # keys x heads x d
+        assert torch.equal(flat[11:20], rows) and not flat[:11].any() and not flat[20:].any()
+        assert not cache[[0, 2, 4, 5]].any()

@@ -289,3 +289,12 @@ def test_a_captured_step(lib):
         got = [t.clone() for t in captured]
         for g, e in zip(got, step()):
             assert torch.equal(g, e)
+
+
+@pytest.mark.parametrize("heads,N", ((0, 5), (4, 0)))
+def test_gradients_of_keys_that_no_query_reads(lib, heads, N):
+    Q, K, V = operands(2, heads, 2, N, 70, 64, 3)
+    O, lse = lib.recurrence_attention_window(Q, K, V)
+    dK, dV = torch.full_like(K, 7.0), torch.full_like(V, 7.0)
+    lib.recurrence_attention_window_grad(Q, K, V, O, lse, torch.ones_like(Q), dK=dK, dV=dV)
+    assert not dK.any() and not dV.any()

@@ -147,3 +147,33 @@ def test_tensors_that_are_refused(pkg):
         pkg.recurrence_attention_paged(x[0], x, x, t, n, s)
     with pytest.raises(ValueError, match="same strides"):
         pkg.recurrence_attention_paged(x[0], x, x.transpose(1, 2), t, n, s)
+
+
+def test_caches_whose_keys_and_values_meet(pkg):
+    """Appending to keys and values that have memory in common is refused.  (False: they lie between one another; the append that this
+    allows is among the tests on the device.)"""
+    row, page = 64 * 2, 2 * 16 * 64 * 2                                       # bytes of cache()'s rows and pages
+    wide = dict(row_stride=128, head_stride=16 * 128, page_stride=2 * 16 * 128)   # keys and values side by side, row by row
+    above = dict(page_stride=2 * 2 * 16 * 64)                                 # page by page
+    for met, at, strides in ((True, row, {}), (True, -row, {}), (True, page, {}), (True, 7 * page, {}), (True, 16, {}), (False, 8 * page, {}),
+                             (False, row, wide), (True, 2 * row, wide), (True, 16, wide), (False, 31 * 2 * row + row, wide), (False, page, above),
+                             (True, 2 * page, above), (True, page - row, above), (True, 3 * page - 16, above), (True, -page + 16, above)):
+        c = cache(pkg, V=K + at, **strides)
+        taken, meet = set(), False
+        for k in (0, 1):
+            for n in range(8 * 2 * 16):
+                first = at * k // 2 + n // 32 * c.page_stride + n // 16 % 2 * c.head_stride + n % 16 * c.row_stride
+                row_of = set(range(first, first + 64, 8))
+                meet |= bool(row_of & taken) if k else False
+                taken |= set() if k else row_of
+        assert meet == met, (at, strides)
+        if met:
+            assert pkg.cyc_cache_append(Q, O, c, 3, None) == ALIAS, (at, strides)
+
+
+def test_gradient_of_keys_without_queries(pkg):
+    assert pkg.cyc_attention_window_grad_workspace(1, 0, 2, 8, 8, 64, 0, 0) == pkg.cyc_attention_window_grad_workspace(1, 2, 2, 0, 8, 64, 0, 0) > 0
+    assert pkg.cyc_attention_window_grad_workspace(1, 0, 0, 8, 8, 64, 0, 0) == 0
+    assert grad(pkg, heads=0, dk=0) == NULL and grad(pkg, heads=0, dv=DK) == ALIAS and grad(pkg, heads=0, size=16) == WORKSPACE
+    assert grad(pkg, heads=0, M=0, q=0, k=0, v=0, o=0, lse=0, do=0, dq=0, dk=0, dv=0) == 0
+    assert grad(pkg, batch=0, kv=1 << 40, heads=1 << 40, M=1 << 29) == 0
