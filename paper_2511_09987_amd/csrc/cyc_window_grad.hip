@@ -45,6 +45,7 @@ template <int PENDING, bool COLUMNS> __device__ __forceinline__ void arrived(Gro
 }
 
 // what is left beside products: nothing, or the elements M * COUNT / MS .. of COUNT beside product M of MS
+template <int N> constexpr std::integral_constant<int, N> number{};
 constexpr auto nothing = [](auto) __attribute__((always_inline)) {};
 template <int COUNT, int MS, int M, class F> __device__ __forceinline__ void share(F &&f)
 {
@@ -146,7 +147,7 @@ template <int D> struct Tile {
 #pragma unroll
                 for (int n = 0; n < NB; ++n)
 #pragma unroll
-                    for (int x = 0; x < 4; ++x) acc[id][n][x] += seen(r, n) & !__builtin_isfinite((float)v[x]) ? add((float)v[x]) : 0.0f;
+                    for (int x = 0; x < 4; ++x) acc[id][n][x] += (seen(r, n) & !__builtin_isfinite((float)v[x])) ? add((float)v[x]) : 0.0f;
             }
         }
     }
@@ -161,6 +162,18 @@ __device__ __forceinline__ int pack(float x, float y)
 
 __device__ __forceinline__ float not_a_number(float) { return __builtin_nanf(""); }
 __device__ __forceinline__ float itself(float x) { return x; }
+
+// Is any of the wave's N sums `sum(i)` no finite number?  (0 times an infinity or NaN is NaN, and stays.)
+template <int N, class Sum> __device__ __forceinline__ bool not_finite(Sum &&sum)
+{
+    float zero = 0;
+    static_for<N>([&](auto i_c) __attribute__((always_inline)) {
+        const f32x4 x = sum(i_c);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) zero = __builtin_fmaf(x[r], 0.0f, zero);
+    });
+    return __builtin_amdgcn_ballot_w64(zero != 0) != 0;
+}
 
 // lse and D of every row by head, lse in the log2 domain, heads padded to whole tiles
 __host__ __device__ inline int64_t padded_rows(int N) { return ((int64_t)N + TILE - 1) / TILE * TILE; }
@@ -381,9 +394,11 @@ struct Runs {
 constexpr int KEY_BLOCKS = 2;            // 16-key blocks of a wave: what the registers hold at d = 128
 constexpr int KEYS = 64 * KEY_BLOCKS;
 
-// The code for tiles that are not all finite takes registers that the usual case does not have to spare (96 of them spilled, and
-// half the speed), so it has a launch of its own: CAREFUL false does without and leaves a mark where it met such a masked tile, CAREFUL true
-// does the marked workgroups again.
+// Masked tiles go through the same stream of groups as whole ones, P and dS set to 0 where a query does not see a key (3 x 12 heads x 1777 x
+// d 64, window 333: 51 us with code of their own, one phase after the other, 40 so).  That 0 times an infinity or NaN in Q or dO is NaN shows
+// in the sums at the end, and the code that keeps those out takes registers that the usual case does not have to spare (96 of them
+// spilled, and half the speed).  So it has a launch of its own: CAREFUL false does without and leaves a mark where its sums are not all
+// finite, CAREFUL true does the marked workgroups again.
 
 // What a workgroup does, with its two stages and the values of its keys in `lds`.
 template <int D> constexpr int STAGE_BYTES = 2 * TILE * D * 2 + 1024;             // the tile of Q, that of dO, lse and D of its rows
@@ -396,7 +411,6 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mark = block * 4;
-    bool marked = false;
     // the short runs of the first tiles before all others
     const int pairs = p.batch * p.kv_heads, in_first = runs.first * runs.first_runs, sinks_end = pairs * in_first;
     const bool early = block < sinks_end;
@@ -426,7 +440,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     const int u_last = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * (run + 1) / nruns));
     int next_head, next_tile;                                        // of the tile to be requested next
     if (u_first < whole_tiles) {
-        next_head = u_first / whole;
+        next_head = u_first / max(whole, 1);
         next_tile = w_first + u_first - next_head * whole;
     } else {
         const int v = u_first - whole_tiles;
@@ -504,14 +518,27 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     i32x4 py[KB], dsy[KB];                                           // P and dS as B operands
     Group x[2];
     // 16 (query, key) pairs a lane; number e: [16-query block][key block][element]
-    auto weigh = [&](auto e_c) __attribute__((always_inline)) {
+    // What a lane's two keys see, as distances in positions: query row r of a tile sees key n if 0 <= p0 + r - key < limit[n], the sinks' limit being
+    // that of the call's last position.  (Rows behind the last query repeat it and see nothing.)
+    int limit[KB], ahead;                                            // ahead: p0 + 4 (l/16) - the first key
+    auto seen = [&](auto c_c, auto n_c, auto r_c) __attribute__((always_inline)) {
+        constexpr int n = decltype(n_c)::value;
+        return (unsigned)(ahead + (decltype(c_c)::value * 16 + decltype(r_c)::value - n * 16)) < (unsigned)limit[n];
+    };
+    auto weigh = [&](auto masked, auto e_c) __attribute__((always_inline)) {
         constexpr int e = decltype(e_c)::value, c = e / 8, n = e / 4 % 2, r = e % 4;
         s[c][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][n][r], scale, -lse[c][r]));
+        if constexpr (decltype(masked)::value) s[c][n][r] = seen(number<c>, number<n>, number<r>) ? s[c][n][r] : 0.0f;
         if constexpr (r % 2 == 1) py[n][c * 2 + r / 2] = pack(s[c][n][r - 1], s[c][n][r]);
     };
-    auto slope = [&](auto e_c) __attribute__((always_inline)) {       // elements 2 e and 2 e + 1
+    auto slope = [&](auto masked, auto e_c) __attribute__((always_inline)) {       // elements 2 e and 2 e + 1
         constexpr int e = 2 * decltype(e_c)::value, c = e / 8, n = e / 4 % 2, r = e % 4;
-        dsy[n][c * 2 + r / 2] = pack(s[c][n][r] * (dp[c][n][r] - Di[c][r]), s[c][n][r + 1] * (dp[c][n][r + 1] - Di[c][r + 1]));
+        float x = s[c][n][r] * (dp[c][n][r] - Di[c][r]), y = s[c][n][r + 1] * (dp[c][n][r + 1] - Di[c][r + 1]);
+        if constexpr (decltype(masked)::value) {
+            x = seen(number<c>, number<n>, number<r>) ? x : 0.0f;
+            y = seen(number<c>, number<n>, number<r + 1>) ? y : 0.0f;
+        }
+        dsy[n][c * 2 + r / 2] = pack(x, y);
     };
     auto read_stats = [&](f32x4(&to)[2], const CYC_LDS char *from) __attribute__((always_inline)) {
 #pragma unroll
@@ -534,8 +561,8 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
         });
     };
     const uint32_t values = T::row_address(lds_base + 2 * STAGE + w * KW * ROW, l);
-    // A tile whose queries all see all keys, as one stream of groups: S, dP beside which P is taken, dV beside which dS is, dK.
-    auto whole_tile = [&](const CYC_LDS char *here) __attribute__((always_inline)) {
+    // A tile as one stream of groups: S, dP beside which P is taken, dV beside which dS is, dK.  masked: not all queries see all keys.
+    auto stream_tile = [&](auto masked, const CYC_LDS char *here) __attribute__((always_inline)) {
         constexpr int NS = DS / 2, NQ = DT / 2, GROUPS = NS + DS + 2 * NQ;
         const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
         auto request = [&](auto n_c) __attribute__((always_inline)) {
@@ -554,11 +581,11 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
             if constexpr (n < NS) T::template multiply_rows<n>(s, x[n % 2], kf, nothing);
             else if constexpr (n < NS + DS) {
                 multiply_values(std::integral_constant<int, n - NS>{}, x[n % 2], [&](auto m_c) __attribute__((always_inline)) {
-                    share<16, 4 * DS, (n - NS) * 4 + decltype(m_c)::value>(weigh);
+                    share<16, 4 * DS, (n - NS) * 4 + decltype(m_c)::value>([&](auto e_c) __attribute__((always_inline)) { weigh(masked, e_c); });
                 });
             } else if constexpr (n < NS + DS + NQ) {
                 T::template multiply_columns<n - NS - DS>(dv, x[n % 2], py, [&](auto m_c) __attribute__((always_inline)) {
-                    share<8, 2 * KB * NQ, (n - NS - DS) * 2 * KB + decltype(m_c)::value>(slope);
+                    share<8, 2 * KB * NQ, (n - NS - DS) * 2 * KB + decltype(m_c)::value>([&](auto e_c) __attribute__((always_inline)) { slope(masked, e_c); });
                 });
             } else T::template multiply_columns<n - NS - DS - NQ>(dk, x[n % 2], dsy, nothing);
         });
@@ -568,6 +595,15 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
         const int p0 = i0 + shift, p1 = (i0 + TILE < N ? i0 + TILE : N) - 1 + shift;
         if (kw >= M || p1 < kw || (kw >= sinks && (int64_t)p0 - kw_last >= window)) return;
         touched = true;
+        if constexpr (!CAREFUL) {
+            const int l = fresh(threadIdx.x & 63);
+            const int key = kw + (l & 15), left = M - key;
+            ahead = p0 + 4 * (l >> 4) - key;
+#pragma unroll
+            for (int n = 0; n < KB; ++n) limit[n] = max(min(left - n * 16, key + n * 16 < sinks ? INT_MAX : window), 0);
+            stream_tile(std::true_type{}, here);
+            return;
+        }
         const bool all = kw_last <= p0 && kw_last < M && i0 + TILE <= N && (p1 - kw < window || kw_last < sinks);
         const int l = fresh(threadIdx.x & 63), g = l >> 4, lq = l & 15;
         const uint32_t row_at = fresh(by_row), column_at = fresh(by_column), v_at = fresh(values);
@@ -606,11 +642,10 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
                 dsy[n][i] = pack(dp[i / 2][n][i % 2 * 2], dp[i / 2][n][i % 2 * 2 + 1]);
             }
         const bool careful = !all && (T::infinite(here, l) || T::infinite(here + TILE_BYTES, l));
-        if (CAREFUL && careful) {
+        if (careful) {
             T::accumulate_carefully(dv, column_at + TILE_BYTES, here + TILE_BYTES, l, py, visible, itself);
             T::accumulate_carefully(dk, column_at, here, l, dsy, visible, not_a_number);
         } else {
-            marked |= careful;
             T::template accumulate<TILE_BYTES>(dv, column_at, py);
             T::template accumulate<0>(dk, column_at, dsy);
         }
@@ -632,7 +667,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     while (u < u_last && u < whole_tiles) {
         arrive();
         touched = true;
-        whole_tile(lds + ((u - u_first) & 1) * STAGE);
+        stream_tile(std::false_type{}, lds + ((u - u_first) & 1) * STAGE);
         leave();
     }
     while (u < u_last) {
@@ -641,7 +676,13 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
         leave();
     }
 
-    if (!CAREFUL && l == 0) marks[mark + w] = marked;
+    if constexpr (!CAREFUL) {
+        const bool marked = not_finite<2 * DT * KB>([&](auto i_c) __attribute__((always_inline)) {
+            constexpr int i = decltype(i_c)::value;
+            return i % 2 ? dk[i / 2 / KB][i / 2 % KB] : dv[i / 2 / KB][i / 2 % KB];
+        });
+        if (l == 0) marks[mark + w] = marked;
+    }
     // accumulator register r of lane l: d = 16 id + 4 (l/16) + r, key kw + 16 n + l%16
     const float back = 1.0f / __builtin_sqrtf((float)D);
 #pragma unroll
