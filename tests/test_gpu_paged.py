@@ -338,3 +338,24 @@ def test_append_to_keys_and_values_in_one_pool(lib, dim):
         flat = torch.cat([cache[3], cache[1]], 1).transpose(0, 1)             # keys x heads x d
         assert torch.equal(flat[11:20], rows) and not flat[:11].any() and not flat[20:].any()
         assert not cache[[0, 2, 4, 5]].any()
+
+
+def test_few_rows_with_runs_beside_many_without(lib):
+    """Many tokens whose keys are not split, and sequences of a few whose are: also one that sees nothing with its first token, one with a
+    wrong length and one that reaches past the last token."""
+    new, lengths, heads, window, sinks = [1, 700, 3, 16, 17, 0, 4, 5, 2], [1500, 900, 1100, 1030, 800, 5, 3, 200, 1200], 64, 1000, 70
+    batch = Batch(new, lengths, heads, heads, 64, 16, 21)
+    out = torch.full(batch.Q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+    lib.recurrence_attention_paged(batch.Q, *batch.arguments(), window=window, sinks=sinks, out=out)
+    batch.check(out, window, sinks)
+    lens, starts = batch.lens.clone(), batch.starts.clone()
+    lens[7] = -1
+    starts[-1] += 3
+    lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, lens, starts, window=window, sinks=sinks, out=out)
+    batch.check(out, window, sinks, only=range(7))
+    assert bool(out[batch.rows[7]:].isnan().all())
+    starts = batch.starts.clone()
+    starts[0] = -3
+    lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, batch.lens, starts, window=window, sinks=sinks, out=out)
+    batch.check(out, window, sinks, only=range(1, 9))
+    assert bool(out[:1].isnan().all())
