@@ -95,14 +95,17 @@ __device__ __forceinline__ int finite_pair(int pair)
 // Which of `pairs` (batch element, key head) and which of its `units` a workgroup takes.  Workgroups go to the eight XCDs round robin by their
 // index and each XCD has its own L2: a pair stays on one XCD, whose 64 places (32 compute units x 2) go through the units of one
 // pair after the other, or of as many side by side as fill them, unit after unit: with the longest units first, those of the last pair
-// would otherwise begin when there is nothing left to run beside them (64 pairs x 32 units of a causal mask, gradient: 945 us, and
-// 896 two by two).  (Fewer than eight pairs share the XCDs, with neighbouring units on different ones, so that the long ones are spread over all.)
+// would otherwise begin when there is nothing left to run beside them (64 pairs x 32 units of a causal mask, gradient: 955 us, and
+// 892 two by two).  (Fewer than eight pairs share the XCDs, with neighbouring units on different ones, so that the long ones are spread over all.)
 struct Place {
     int pair, unit;
     __device__ __forceinline__ Place(int at, int pairs, int units)
     {
-        const int together = 8 * ((63 + units) / units), base = at / (together * units) * together;
-        const int side = pairs - base < together ? pairs - base : together, local = at - base * units;
+        // pairs in groups of `together`, then as many eights of them as are left, then the rest
+        const int together = 8 * ((63 + units) / units), full = pairs / together * together, eights = pairs / 8 * 8;
+        const int start = at / units;                                // (of the pairs before: a group's workgroups follow one another)
+        const int base = start < full ? start / together * together : start < eights ? full : eights;
+        const int side = start < full ? together : start < eights ? eights - full : pairs - eights, local = at - base * units;
         unit = local / side;
         pair = base + local - unit * side;
     }
