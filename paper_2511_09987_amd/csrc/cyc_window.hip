@@ -31,13 +31,13 @@ struct TileProblem {
     int batch, kv_heads, group, N, M;                                // paged: batch = sequences, N and M by sequence
     int tiles;                                                       // tiles of rows (paged, long sequences: of all of them together)
     int tokens, pages, page_shift, max_pages, max_new, short_rows;
-    int window, sinks, splits, run_tiles;                            // runs of keys: how many, tiles in each
+    int window, sinks, splits, run_tiles;                            // runs of keys: how many, and, few rows of sequences in pages, tiles in each at most
     float scale_log2e;
     // what a run leaves: part[run][row][d], refs[run][row][2].  Rows are those of O, (token or query, head) pairs, or, in launches for few rows,
     // SHORT_ROWS for each (problem, key head)
     float *part, *refs;
     int64_t part_rows, rows;                                         // rows of a run there; rows of O
-    // paged, long sequences: splits is the most runs there may be, *chosen receives how many there are, none of more than most_tiles / runs tiles
+    // paged, long sequences: splits is the most runs there may be, *chosen receives how many there are; most_tiles: of any list
     int *chosen;
     int most_tiles;
 };
@@ -67,6 +67,7 @@ __device__ __forceinline__ int most_keys(const int *lengths, int seqs)
 // sequence and, for one tile, which sequence it belongs to and which of its tiles it is.
 struct Tiles {
     int total = 0, keys = 0, seq = -1, tile = 0;
+    int upto = 0, own = 0;                                 // of the last 64: tiles up to this lane's sequence, and its own
     // all: look at all sequences (total and keys are right then), not only up to the tile's
     __device__ __forceinline__ void find(const TileProblem &p, int per, int slot, bool all)
     {
@@ -80,33 +81,39 @@ struct Tiles {
             end = end < first ? first : end > p.tokens ? p.tokens : end;
             const int rows = (end - first) * p.group, tiles = rows > p.short_rows ? (rows + per - 1) / per : 0;
             most = tiles > 0 && length > most ? length : most;
-            int upto = tiles;                              // of the sequences b0 .. b
+            own = upto = tiles;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
                 const int below = __shfl_up(upto, d);
                 upto += l >= d ? below : 0;
             }
-            const uint64_t past = __builtin_amdgcn_ballot_w64(total + upto > slot);
-            if (past && seq < 0) {
-                const int at = __builtin_ctzll(past);
-                seq = b0 + at;
-                tile = slot - total - __builtin_amdgcn_readlane(upto - tiles, at);
-            }
+            pick(b0, slot);
             total += __builtin_amdgcn_readlane(upto, 63);
         }
         if (all) keys = wave_most(most);
+    }
+    // the slot's tile, if it is one of the last 64 sequences, the first of which is b0
+    __device__ __forceinline__ void pick(int b0, int slot)
+    {
+        const uint64_t past = __builtin_amdgcn_ballot_w64(total + upto > slot);
+        if (past == 0 || seq >= 0) return;
+        const int at = __builtin_ctzll(past);
+        seq = b0 + at;
+        tile = slot - total - __builtin_amdgcn_readlane(upto - own, at);
     }
 };
 
 // Many rows: the time in nanoseconds of `groups` workgroups, each walking up to `tiles` tiles of keys, that are cut into `runs` runs each.  The chip
 // holds 512, two on a compute unit, which take 1900 ns a tile of 64 keys x 128 rows x d 128 together (128 keys x d 64: 3100, twice the
 // weights), or 1650 (2600) where there is one; to start takes 4 us.  Runs add a launch and the partial outputs, which are written and read
-// at 3 TB/s.  (1024 + 7 x 1 tokens behind 6800 keys, 8 key heads, 256 workgroups: one run 215 us, three 158, two 120.)
-__host__ __device__ inline int64_t long_cost(int64_t groups, int64_t tiles, int64_t runs, int64_t rows, int64_t d)
+// at 3 TB/s.  (1024 + 7 x 1 tokens behind 6800 keys, 8 key heads, 256 workgroups: one run 209 us, two 147.)
+__host__ __device__ inline int64_t part_time(int64_t rows, int64_t d) { return rows * (d + 2) * 4 / 3000; }      // of a run
+__host__ __device__ inline int64_t long_cost(int groups, int tiles, int runs, int64_t part, int d)
 {
-    const int64_t all = groups * runs, full = all / 512, rest = all % 512, length = (tiles + runs - 1) / runs;
-    const int64_t two = (d == 128 ? 1900 : 3100) * length + 4000, one = (d == 128 ? 1650 : 2600) * length + 4000;
-    return full * two + (rest == 0 ? 0 : rest <= 256 ? one : two) + (runs > 1 ? 6000 + rows * (d + 2) * 4 * runs / 3000 : 0);
+    // (32-bit divisions: every workgroup of a paged call does this)
+    const unsigned all = (unsigned)groups * runs, full = all / 512, rest = all % 512, length = (unsigned)(tiles + runs - 1) / runs;
+    const int64_t two = (int64_t)(d == 128 ? 1900 : 3100) * length + 4000, one = (int64_t)(d == 128 ? 1650 : 2600) * length + 4000;
+    return full * two + (rest == 0 ? 0 : rest <= 256 ? one : two) + (runs > 1 ? 6000 + part * runs : 0);
 }
 
 // D: head dimension; KT: keys per tile; NWAVE waves of QB * 16 rows.
@@ -159,27 +166,32 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             // Likewise, and how many runs is decided here too, where the number of tiles of rows is known.  All workgroups that have work come
             // first: 504 of them fill the chip's 512 places as long as none is held by one that only finds nothing to do.
             Tiles rows;
-            int work = blockIdx.x / p.kv_heads;
+            const int work = blockIdx.x / p.kv_heads, splits_most = splits;
             if (splits > 1) {
-                rows.find(p, ROWS, -1, true);
+                rows.find(p, ROWS, INT_MAX, true);
                 const int most = (rows.keys + KT - 1) / KT, tiles = most < p.most_tiles ? most : p.most_tiles;
-                int64_t best = long_cost((int64_t)rows.total * p.kv_heads, tiles, 1, p.rows, D);
+                const int64_t part = part_time(p.rows, D);
+                int64_t best = long_cost(rows.total * p.kv_heads, tiles, 1, part, D);
                 int runs = 1;
                 for (int r = 2; r <= splits && r * 4 <= tiles; ++r) {
-                    const int64_t cost = long_cost((int64_t)rows.total * p.kv_heads, tiles, r, p.rows, D);
+                    const int64_t cost = long_cost(rows.total * p.kv_heads, tiles, r, part, D);
                     runs = cost < best ? r : runs;
                     best = cost < best ? cost : best;
                 }
                 splits = __builtin_amdgcn_readfirstlane(runs);
-                run_tiles = __builtin_amdgcn_readfirstlane((tiles + runs - 1) / runs);
                 if (blockIdx.x == 0 && threadIdx.x == 0) *p.chosen = splits;
             }
             // (eight neighbours, whose key heads are different or whose tiles follow one another, run on the eight XCDs)
             head = blockIdx.x - work * p.kv_heads;
             const int slot = work / splits;
             run = work - slot * splits;
-            rows = Tiles();
-            rows.find(p, ROWS, slot, false);
+            if (splits_most > 1 && p.batch <= 64) {
+                rows.total = 0;                            // (one look at the sequences was enough)
+                rows.pick(0, slot);
+            } else {
+                rows = Tiles();
+                rows.find(p, ROWS, slot, false);
+            }
             if (rows.seq < 0) return;
             b = rows.seq;
             tile = rows.tile;
@@ -217,6 +229,11 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
     // ---- the keys that the rows of the workgroup see, and this run's share of their tiles (none, if the list ends before)
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
     const KeyList<KT> list(row_first, row_last, group, N, M, window, sinks);
+    if (A != PAGED_SHORT && splits > 1) {
+        // equal runs of what these rows see, which need not be what others see
+        run_tiles = (int)((unsigned)(list.count + splits - 1) / (unsigned)splits);
+        run_tiles = run_tiles < 4 ? 4 : run_tiles;
+    }
     const int u_first = run * run_tiles, left = list.count - u_first;
     const int ntiles = left < run_tiles || run == splits - 1 ? left : run_tiles;
     auto tile_key = [&](int u) __attribute__((always_inline)) { return list.tile_key(u + u_first); };
@@ -712,8 +729,11 @@ constexpr int MOST_RUNS = 16;
 Runs choose_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
 {
     int64_t best = 1;
-    for (int64_t r = 2; r <= MOST_RUNS && r * 4 <= tiles && rows * (d + 2) * 4 * r <= MOST_PART; ++r)
-        if (long_cost(groups, tiles, r, rows, d) < long_cost(groups, tiles, best, rows, d)) best = r;
+    const int64_t part = part_time(rows, d);
+    auto cost = [&](int64_t r) { return long_cost((int)groups, (int)tiles, (int)r, part, (int)d); };
+    if (groups * MOST_RUNS < (1 << 30))
+        for (int64_t r = 2; r <= MOST_RUNS && r * 4 <= tiles && rows * (d + 2) * 4 * r <= MOST_PART; ++r)
+            if (cost(r) < cost(best)) best = r;
     return runs_of(tiles, best);
 }
 // Sequences in pages: the device decides (tile_kernel) and needs a grid and memory for what it may choose.  Runs come into question below four
