@@ -7,6 +7,15 @@ namespace cyc {
 // Key j is visible to position p: the sinks and the last `window` positions up to p itself (window INT_MAX: all of them).
 __host__ __device__ inline bool sees(int p, int j, int window, int sinks) { return j <= p && (p - j < window || j < sinks); }
 
+// How long `all` equal workgroups take, of which a compute unit holds two: `two` (any unit) a round of 512, `one` where there are 256 or fewer.
+__host__ __device__ inline int64_t rounds_time(unsigned all, int64_t two, int64_t one)
+{
+    const unsigned rest = all % 512;
+    return all / 512 * two + (rest == 0 ? 0 : rest <= 256 ? one : two);
+}
+// Tiles of kt keys that `rows` rows, of `group` heads at `queries` positions or fewer, see at most among `keys`.
+int64_t most_tiles(int64_t keys, int window, int sinks, int64_t rows, int64_t group, int64_t queries, int64_t kt);
+
 // batch x heads x rows, row by row of d bfloat16; strides in bytes
 struct Strided {
     const char *base;

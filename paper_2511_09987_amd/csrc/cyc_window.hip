@@ -111,9 +111,9 @@ __host__ __device__ inline int64_t part_time(int64_t rows, int64_t d) { return r
 __host__ __device__ inline int64_t long_cost(int groups, int tiles, int runs, int64_t part, int d)
 {
     // (32-bit divisions: every workgroup of a paged call does this)
-    const unsigned all = (unsigned)groups * runs, full = all / 512, rest = all % 512, length = (unsigned)(tiles + runs - 1) / runs;
+    const unsigned length = (unsigned)(tiles + runs - 1) / runs;
     const int64_t two = (int64_t)(d == 128 ? 1900 : 3100) * length + 4000, one = (int64_t)(d == 128 ? 1650 : 2600) * length + 4000;
-    return full * two + (rest == 0 ? 0 : rest <= 256 ? one : two) + (runs > 1 ? 6000 + part * runs : 0);
+    return rounds_time((unsigned)groups * runs, two, one) + (runs > 1 ? 6000 + part * runs : 0);
 }
 
 // D: head dimension; KT: keys per tile; NWAVE waves of QB * 16 rows.
@@ -746,13 +746,6 @@ Runs most_long(int64_t groups, int64_t tiles, int64_t rows, int64_t d)
     return {(int)std::max<int64_t>(most, 1), (int)tiles};
 }
 
-// Tiles of kt keys that a workgroup's rows, `rows` of them at `queries` positions or fewer, see at most among `keys`.
-int64_t most_tiles(int64_t keys, int window, int sinks, int64_t rows, int64_t group, int64_t queries, int64_t kt)
-{
-    const int64_t span = window + std::min(queries, (rows - 1) / group + 2);
-    return std::min((keys + kt - 1) / kt, (std::min<int64_t>(span, keys) + kt - 1) / kt + 1 + (std::min<int64_t>(sinks, keys) + kt - 1) / kt);
-}
-
 Mapping window_mapping(const WindowProblem &p)
 {
     const int64_t R = (int64_t)p.N * p.group, pairs = (int64_t)p.batch * p.kv_heads, rows = R * pairs;
@@ -813,6 +806,12 @@ template <int D, bool PAGED> hipError_t launch_tiles(TileProblem t, Mapping m, v
 }
 
 }  // namespace
+
+int64_t most_tiles(int64_t keys, int window, int sinks, int64_t rows, int64_t group, int64_t queries, int64_t kt)
+{
+    const int64_t span = window + std::min(queries, (rows - 1) / group + 2);
+    return std::min((keys + kt - 1) / kt, (std::min<int64_t>(span, keys) + kt - 1) / kt + 1 + (std::min<int64_t>(sinks, keys) + kt - 1) / kt);
+}
 
 int64_t window_workspace_bytes(const WindowProblem &p) { return workspace_bytes_of(window_mapping(p), p.d); }
 

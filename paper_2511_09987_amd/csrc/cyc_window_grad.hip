@@ -179,10 +179,11 @@ template <int N, class Sum> __device__ __forceinline__ bool not_finite(Sum &&sum
 __host__ __device__ inline int64_t padded_rows(int N) { return ((int64_t)N + TILE - 1) / TILE * TILE; }
 
 // ---- dQ.  A workgroup of four waves keeps 128 rows r (query r / group, head r % group of a key head) and walks the keys that any of them
-// sees in tiles of 64, two steps of 32 to a barrier.  Also writes lse and D of its rows for the other kernel.
-constexpr int KEY_TILE = 64;
+// sees in tiles of 64, two steps of 32 to a barrier.  Also writes lse and D of its rows for the other kernel.  Where there are few workgroups, each
+// list of keys is cut into runs, which different workgroups take and the last kernel adds up.
+constexpr int KEY_TILE = 64, LEAST_TILES = 4;   // of a run
 
-template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const WindowProblem p, int tiles, float scale, float *lse2, float *Ds)
+template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const WindowProblem p, int tiles, int runs, float scale, float *lse2, float *Ds, float *part)
 {
     typedef Tile<D> T;
     constexpr int ROW = T::ROW, CPR = T::CPR, DS = T::DS, DT = T::DT, QB = 2, QW = 32, ROWS = 128;
@@ -191,8 +192,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
     CYC_LDS char *lds = (CYC_LDS char *)lds_raw;
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Place at(blockIdx.x, p.batch * p.kv_heads, tiles);
-    const int tile = tiles - 1 - at.unit;                                           // (the most keys first)
+    const Place at(blockIdx.x, p.batch * p.kv_heads, tiles * runs);
+    const int run = at.unit % runs, tile = tiles - 1 - at.unit / runs;              // (the most keys first)
     const int64_t b = at.pair / p.kv_heads;
     const int head = at.pair - (int)b * p.kv_heads;
     const int group = p.group, N = p.N, M = p.M, R = N * group, window = p.window, sinks = p.sinks;
@@ -201,7 +202,8 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
 
     const int row_first = tile * ROWS, row_last = (R - row_first < ROWS ? R : row_first + ROWS) - 1;
     const KeyList<KEY_TILE> list(row_first, row_last, group, N, M, window, sinks);
-    const int ntiles = list.count;
+    const int per = runs == 1 ? list.count : max((list.count + runs - 1) / runs, LEAST_TILES);
+    const int u_first = run * per, u_last = run == runs - 1 || u_first + per > list.count ? list.count : u_first + per;
 
     const int r0 = row_first + w * QW;
     const bool idle = r0 > row_last;
@@ -233,7 +235,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
         Di[jq] = query_sum(dot);
         const int64_t row = b * p.heads + h;
         lse[jq] = p.lse[row * N + i] * 1.4426950408889634f;
-        if (mine && g == 0) {
+        if (mine && g == 0 && run == 0) {
             lse2[row * padded_rows(N) + i] = lse[jq];
             Ds[row * padded_rows(N) + i] = Di[jq];
         }
@@ -243,7 +245,7 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
     const bool small_strides = k_row < MOST_STRIDE && v_row < MOST_STRIDE;
     auto issue = [&](int u) __attribute__((always_inline)) {
         const int k0 = list.tile_key(u);
-        const uint32_t dst = lds_base + (u & 1) * TILE_BYTES;
+        const uint32_t dst = lds_base + ((u - u_first) & 1) * TILE_BYTES;
         if (small_strides && list.inside(k0)) {
             Copies::whole(K + k0 * k_row, k_row, dst, w, l, swizzle<CPR>);
             Copies::whole(V + k0 * v_row, v_row, dst + 2 * TILE_BYTES, w, l, swizzle<CPR>);
@@ -337,26 +339,26 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
             else T::template accumulate<0>(acc, column_at, y[0]);
         }
     };
-    if (ntiles > 0) issue(0);
-    int u = 0;
+    if (u_first < u_last) issue(u_first);
+    int u = u_first;
     auto arrive = [&]() __attribute__((always_inline)) {
         landed_barrier();
-        if (u + 1 < ntiles) issue(u + 1);
+        if (u + 1 < u_last) issue(u + 1);
     };
     auto leave = [&]() __attribute__((always_inline)) {
-        const int turn = u & 1 ? -TILE_BYTES : TILE_BYTES;
+        const int turn = (u - u_first) & 1 ? -TILE_BYTES : TILE_BYTES;
         by_row += turn;
         by_column += turn;
         ++u;
     };
-    while (u < list.whole) {                                         // (see tile_kernel: a loop for each kind of tile)
+    while (u < u_last && u < list.whole) {                                         // (see tile_kernel: a loop for each kind of tile)
         arrive();
         if (!idle) whole_tile();
         leave();
     }
-    while (u < ntiles) {
+    while (u < u_last) {
         arrive();
-        some_of_tile(list.tile_key(u), u & 1);
+        some_of_tile(list.tile_key(u), (u - u_first) & 1);
         leave();
     }
 
@@ -366,6 +368,12 @@ template <int D> __global__ __launch_bounds__(256, 2) void grad_q_kernel(const W
         const int r = r0 + jq * 16 + lq;
         if (r > row_last) continue;
         const int i = r / group, h = head * group + r - i * group;
+        if (runs > 1) {
+            float *to = part + (((int64_t)run * p.batch * p.heads + b * p.heads + h) * N + i) * D + 4 * g;
+#pragma unroll
+            for (int id = 0; id < DT; ++id) *(f32x4 *)(to + id * 16) = acc[id][jq];
+            continue;
+        }
         char *dq = (char *)p.dQ.base + b * p.dQ.batch + h * p.dQ.head + i * p.dQ.row;
 #pragma unroll
         for (int id = 0; id < DT; ++id) {
@@ -737,11 +745,29 @@ __global__ __launch_bounds__(256, 2) void grad_kv_careful_kernel(const WindowPro
     }
 }
 
-// Adds the runs of a tile of keys in ascending order, those in which the keys' wave did anything; a thread takes four d of a key's dK and dV.
+// Adds the runs in ascending order, a thread four d of a row.  The first workgroups: of a tile of keys, dK and dV, those runs in which the keys' wave did
+// anything; the others: of dQ.
 constexpr int MOST_RUNS = 256;
-template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, const float *part, const int *used)
+template <int D>
+__global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, const Runs runs, int q_runs, const float *part, const int *used, const float *q_part)
 {
-    constexpr int PER = 1024 / D;                                     // keys of a workgroup, all of one wave of the other kernel
+    constexpr int PER = 1024 / D;                                     // keys of a workgroup, all of one wave of the other kernel; rows of dQ
+    const float back = 1.0f / __builtin_sqrtf((float)D);
+    const int of_keys = p.batch * p.kv_heads * runs.kept_tiles() * (KEYS / PER);
+    if ((int)blockIdx.x >= of_keys) {
+        const int64_t rows = (int64_t)p.batch * p.heads * p.N, row = (int64_t)(blockIdx.x - of_keys) * PER + threadIdx.x / (D / 4);
+        const int d = threadIdx.x % (D / 4) * 4;
+        if (row >= rows) return;
+        f32x4 dq = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int x = 0; x < q_runs; ++x) dq += *(const f32x4 *)(q_part + (x * rows + row) * D + d);
+        const int64_t pair = row / p.N;
+        bf16x4 o;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) o[r] = (__bf16)(dq[r] * back);
+        *(bf16x4 *)((char *)p.dQ.base + pair / p.heads * p.dQ.batch + pair % p.heads * p.dQ.head + row % p.N * p.dQ.row + d * 2) = o;
+        return;
+    }
     __shared__ int list[MOST_RUNS], counts[4];
     const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int64_t block = blockIdx.x / (KEYS / PER);                   // (pair, tile)
@@ -770,7 +796,6 @@ template <int D> __global__ __launch_bounds__(256) void grad_join_kernel(const W
         dk += *(const f32x4 *)run;
         dv += *(const f32x4 *)(run + KEYS * D);
     }
-    const float back = 1.0f / __builtin_sqrtf((float)D);
     bf16x4 u, v;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -822,47 +847,68 @@ Runs choose_runs(const WindowProblem &p)
     return best;
 }
 
+// How the keys of a tile of rows are cut.  A tile of 64 keys x 128 rows x d 128 takes two workgroups on a compute unit 2800 ns, a lone one 1600
+// (d 64: 1800, 1200); each run brings partial sums, and all together the join (8 heads x 100 x 8192 x 128: one run 204 us, 26
+// 17 and the join 4; one head x 8192 x 8192 x 128 199, and 55 and 9).
+int row_runs(const WindowProblem &p)
+{
+    const int64_t groups = (int64_t)p.batch * p.kv_heads * (((int64_t)p.N * p.group + 127) / 128), rows = (int64_t)p.batch * p.heads * p.N;
+    const int64_t tiles = most_tiles(p.M, p.window, p.sinks, 128, p.group, p.N, KEY_TILE);
+    auto cost = [&](int64_t r) {
+        const int64_t length = (tiles + r - 1) / r, two = (p.d == 128 ? 2800 : 1800) * length + 4000, one = (p.d == 128 ? 1600 : 1200) * length + 4000;
+        return rounds_time((unsigned)(groups * r), two, one) + (r > 1 ? 4000 + rows * p.d * 8 * r / 3000 : 0);
+    };
+    int64_t best = 1;
+    if (groups < (1 << 20))
+        for (int64_t r = 2; r <= 32 && r * LEAST_TILES <= tiles && rows * p.d * 4 * r <= MOST_PART / 2; ++r)
+            if (cost(r) < cost(best)) best = r;
+    return (int)best;
+}
+
 int64_t stats_bytes(const WindowProblem &p) { return ((int64_t)p.batch * p.heads * padded_rows(p.N) * 8 + 255) / 256 * 256; }
 
 // Where a call keeps what in its workspace, in bytes.
 struct Layout {
-    int64_t marks, used, part, end;
-    Layout(const WindowProblem &p, const Runs &runs)
+    int64_t marks, used, part, q_part, end;
+    Layout(const WindowProblem &p, const Runs &runs, int q_runs)
     {
         const int64_t pairs = p.M > 0 ? (int64_t)p.batch * p.kv_heads : 0;
         marks = stats_bytes(p);
         used = marks + pairs * runs.per_pair() * 16;
         part = used + pairs * runs.kept_per_pair() * 16;
-        end = part + pairs * runs.kept_per_pair() * 2 * KEYS * p.d * 4;
+        q_part = part + pairs * runs.kept_per_pair() * 2 * KEYS * p.d * 4;
+        end = q_part + (q_runs > 1 ? (int64_t)p.batch * p.heads * p.N * p.d * 4 * q_runs : 0);
     }
 };
 
 template <int D> hipError_t launch_grad(const WindowProblem &p, void *workspace, hipStream_t s)
 {
     const Runs runs = choose_runs(p);
-    const Layout at(p, runs);
+    const int q_runs = row_runs(p);
+    const Layout at(p, runs, q_runs);
     char *mem = (char *)workspace;
-    float *lse2 = (float *)mem, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)(mem + at.part);
+    float *lse2 = (float *)mem, *Ds = lse2 + (int64_t)p.batch * p.heads * padded_rows(p.N), *part = (float *)(mem + at.part), *q_part = (float *)(mem + at.q_part);
     int *marks = (int *)(mem + at.marks), *used = (int *)(mem + at.used);
     const float scale = (float)(1.4426950408889634 / __builtin_sqrt((double)D));
     const int tiles = (int)(((int64_t)p.N * p.group + 127) / 128);
     const int64_t pairs = (int64_t)p.batch * p.kv_heads, blocks = runs.per_pair() * pairs;
-    if (tiles * pairs >= ((int64_t)1 << 31) || blocks >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
+    if (tiles * pairs * q_runs >= ((int64_t)1 << 31) || blocks >= ((int64_t)1 << 31)) return hipErrorInvalidValue;
     hipError_t e = hipSuccess;
-    if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs)), dim3(256), s, p, tiles, scale, lse2, Ds);
+    if (p.N > 0) e = launch_kernel(grad_q_kernel<D>, dim3((unsigned)(tiles * pairs * q_runs)), dim3(256), s, p, tiles, q_runs, scale, lse2, Ds, q_part);
     if (e != hipSuccess || p.M == 0) return e;
     auto keys_of = [&](auto kernel, int64_t grid) {
         return launch_kernel(kernel, dim3((unsigned)grid), dim3(256), s, p, runs, scale, (const float *)lse2, (const float *)Ds, part, used, marks);
     };
     e = keys_of(grad_kv_kernel<D>, blocks);
     if (e == hipSuccess) e = keys_of(grad_kv_careful_kernel<D>, std::min<int64_t>(blocks, 256));
-    if (e != hipSuccess || runs.kept_tiles() == 0) return e;
-    return launch_kernel(grad_join_kernel<D>, dim3((unsigned)(pairs * runs.kept_tiles() * (KEYS * D / 1024))), dim3(256), s, p, runs, (const float *)part, (const int *)used);
+    const int64_t of_keys = pairs * runs.kept_tiles() * (KEYS * D / 1024), of_rows = q_runs > 1 ? ((int64_t)p.batch * p.heads * p.N * D + 1023) / 1024 : 0;
+    if (e != hipSuccess || of_keys + of_rows == 0) return e;
+    return launch_kernel(grad_join_kernel<D>, dim3((unsigned)(of_keys + of_rows)), dim3(256), s, p, runs, q_runs, (const float *)part, (const int *)used, (const float *)q_part);
 }
 
 }  // namespace
 
-int64_t window_grad_workspace_bytes(const WindowProblem &p) { return Layout(p, choose_runs(p)).end; }
+int64_t window_grad_workspace_bytes(const WindowProblem &p) { return Layout(p, choose_runs(p), row_runs(p)).end; }
 
 hipError_t launch_window_grad(const WindowProblem &p, void *workspace, int64_t, hipStream_t s)
 {

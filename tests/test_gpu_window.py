@@ -298,3 +298,13 @@ def test_gradients_of_keys_that_no_query_reads(lib, heads, N):
     dK, dV = torch.full_like(K, 7.0), torch.full_like(V, 7.0)
     lib.recurrence_attention_window_grad(Q, K, V, O, lse, torch.ones_like(Q), dK=dK, dV=dV)
     assert not dK.any() and not dV.any()
+
+
+@pytest.mark.parametrize("case", [(1, 4, 2, 300, 2100, 64, None, 0), (2, 3, 1, 65, 1500, 128, 700, 70), (1, 2, 2, 1300, 1300, 128, None, 0),
+                                  (1, 1, 1, 1, 700, 64, 600, 3), (1, 6, 2, 900, 800, 64, 620, 1)], ids=str)
+def test_gradients_of_few_rows_against_many_keys(lib, case):
+    """The keys of a row are cut into runs, as its queries' are."""
+    test_gradient(lib, case)
+    batch, heads, kv, N, M, d, window, sinks = case
+    whole, less = (lib.cyc_attention_window_grad_workspace(batch, heads, kv, n, M, d, window or 0, sinks) for n in (N, 0))
+    assert whole - less > batch * heads * N * d * 4                                # of two runs and more
