@@ -4,8 +4,10 @@
 //     dQ_i = sum_j dS_ij K_j / sqrt(d),   dK_j = sum_i dS_ij Q_i / sqrt(d),   dV_j = sum_i P_ij dO_i,
 // the last two also over the heads that share key j.  Two kernels, so that every sum stays with one owner and no atomic adds are needed:
 // one keeps rows (query, head) and walks their keys for dQ (three products a pair), the other keeps keys and walks the rows that
-// see them for dK and dV (four); P is taken again in the second.  Seven products for the five of the formulas, against the
-// 4 d bytes per pair that P and dS would cost in memory.
+// see them for dK and dV (four); P is taken again in the second.  Seven products for the five of the formulas, against the 4 bytes per
+// pair that P and dS would cost in memory, written and read: about the time of the two products, and room that grows with N M.
+// Bounded by matrix and vector work at the clock that the power limit leaves (2.05 GHz): 4 x 16 heads x 4096 x 128, causal, dQ 362 us, dK and
+// dV 512, 1.1 PFLOP/s of products; 2 x 32/8 heads, window 1024, 200 and 312.
 //
 // Rows (resp. keys) stay in MFMA operand registers, as in cyc_window.hip, and the other side streams through LDS in tiles that are read
 // in two ways: row by row (16 bytes of a row per lane) for the products along d, transposed for those along rows or keys.  The
@@ -807,7 +809,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, c
 }
 
 // How the rows of a tile of keys are cut.  The chip takes 512 workgroups at a time, which count in rounds: 496 and 64 of the same length last
-// twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so, 291 now).  The tiles of sinks, whose rows are all that
+// twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so, 312 now).  The tiles of sinks, whose rows are all that
 // follow, go first in many short runs, which fill what the others leave over; those are cut where that makes fewer or shorter
 // rounds, at a cost: three steps of 32 rows to start a run, the partial sums, written and read, and a launch.
 constexpr int64_t MOST_PART = 128 << 20;
