@@ -733,17 +733,21 @@ __global__ __launch_bounds__(256, 2) void grad_kv_kernel(const WindowProblem p, 
     __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
     keys_of_block<D, false>(p, runs, scale, lse2, Ds, part, used, marks, blockIdx.x, (CYC_LDS char *)lds);
 }
-// a few workgroups look through all marks
+// a few workgroups look through all marks, a lane at one
 template <int D>
 __global__ __launch_bounds__(256, 2) void grad_kv_careful_kernel(const WindowProblem p, const Runs runs, float scale, const float *lse2, const float *Ds, float *part, int *used, int *marks)
 {
     __shared__ __attribute__((aligned(1024))) char lds[KEYS_LDS<D>];
-    const int blocks = p.batch * p.kv_heads * runs.per_pair();
-    for (int block = blockIdx.x; block < blocks; block += gridDim.x) {
-        const i32x4 m = ((const i32x4 *)marks)[block];
-        if ((m[0] | m[1] | m[2] | m[3]) == 0) continue;
-        keys_of_block<D, true>(p, runs, scale, lse2, Ds, part, used, marks, block, (CYC_LDS char *)lds);
-        landed_barrier();                                             // (LDS is free again)
+    const int64_t blocks = (int64_t)p.batch * p.kv_heads * runs.per_pair(), step = gridDim.x;
+    for (int64_t first = blockIdx.x; first < blocks; first += 64 * step) {
+        const int64_t mine = first + (threadIdx.x & 63) * step;
+        i32x4 m = {0, 0, 0, 0};
+        if (mine < blocks) m = ((const i32x4 *)marks)[mine];
+        for (uint64_t todo = __builtin_amdgcn_ballot_w64((m[0] | m[1] | m[2] | m[3]) != 0); todo; todo &= todo - 1) {
+            const int block = (int)(first + __builtin_ctzll(todo) * step);
+            keys_of_block<D, true>(p, runs, scale, lse2, Ds, part, used, marks, block, (CYC_LDS char *)lds);
+            landed_barrier();                                         // (LDS is free again)
+        }
     }
 }
 

@@ -308,3 +308,27 @@ def test_gradients_of_few_rows_against_many_keys(lib, case):
     batch, heads, kv, N, M, d, window, sinks = case
     whole, less = (lib.cyc_attention_window_grad_workspace(batch, heads, kv, n, M, d, window or 0, sinks) for n in (N, 0))
     assert whole - less > batch * heads * N * d * 4                                # of two runs and more
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_queries_that_are_no_numbers_among_many_heads(lib, d):
+    """One query of three of 64 heads, far apart: what does not meet them stays what it is, in their heads and in all others."""
+    N, window, sinks, where = 700, 100, 3, ((0, 0, 650), (2, 7, 90), (3, 15, 699))
+    Q, K, V = operands(4, 16, 16, N, N, d, 51)
+    dO = normal(Q.shape, 52)
+    O, lse = lib.recurrence_attention_window(Q, K, V, window, sinks)
+    want, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    seen = ref.visible(N, N, window, sinks, DEV)
+    for x in (Q, dO):
+        kept = x.clone()
+        for b, h, i in where:
+            x[b, h, i] = float("inf")
+        dQ, dK, dV = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, window, sinks)
+        x.copy_(kept)
+        clean = [torch.ones(t.shape[:3], dtype=torch.bool, device=DEV) for t in (dQ, dK)]
+        for b, h, i in where:
+            clean[0][b, h, i] = False
+            clean[1][b, h, seen[i]] = False
+            assert not torch.isfinite(dK[b, h, i]).any()
+        for g, w, e, c, name in zip((dQ, dK, dV), want, bounds, (clean[0], clean[1], clean[1]), ("dQ", "dK", "dV")):
+            ref.within(g[c], w[c], e[c], name)
