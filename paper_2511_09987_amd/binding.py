@@ -515,6 +515,12 @@ def _dense(t, shape, device, bfloat16) -> bool:
     return t.is_cuda and t.dtype is bfloat16 and t.is_contiguous() and t.shape == shape and t.get_device() == device and not t.data_ptr() & 15
 
 
+def _empty_like(t):
+    """A dense tensor of the shape, type and device of t: empty_like, the faster call by 0.5 of 12 us, would keep other strides."""
+    import torch
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 def _check_rows(name, t, shape, device):
     """A bfloat16 tensor of `shape` on `device` whose rows a kernel can read 16 bytes at a time."""
     import torch
@@ -583,7 +589,7 @@ def _attention_window(Q, K, V, window, sinks, out, lse, stream):
     kv_heads, M = k[1:3]
     device = _device_of("Q", Q)
     if out is None:
-        out = Q.new_empty(q)
+        out = _empty_like(Q)
     strides = _operands((("Q", Q, q), ("K", K, k), ("V", V, k), ("out", out, q)), device)
     if lse is None:
         lse = Q.new_empty(q[:3], dtype=torch.float32)
@@ -620,9 +626,9 @@ def _attention_window_grad(Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV, strea
     batch, heads, N, d = q
     kv_heads, M = k[1:3]
     device = _device_of("Q", Q)
-    dQ = Q.new_empty(q) if dQ is None else dQ
-    dK = Q.new_empty(k) if dK is None else dK
-    dV = Q.new_empty(k) if dV is None else dV
+    dQ = _empty_like(Q) if dQ is None else dQ
+    dK = _empty_like(K) if dK is None else dK
+    dV = _empty_like(V) if dV is None else dV
     strides = _operands((("Q", Q, q), ("K", K, k), ("V", V, k), ("O", O, q), ("dO", dO, q), ("dQ", dQ, q), ("dK", dK, k), ("dV", dV, k)), device)
     _check_lse(lse, q[:3], device)
     s = _stream_handle(Q, stream)
@@ -710,7 +716,7 @@ def _attention_paged(Q, K_cache, V_cache, table, lengths, starts, window, sinks,
     if cache.kv_heads == 0 or heads % cache.kv_heads:
         raise ValueError(f"{heads} query heads do not divide among {cache.kv_heads} key heads")
     if out is None:
-        out = Q.new_empty(q)
+        out = _empty_like(Q)
     strides = _operands((("Q", Q, q), ("out", out, q)), device)
     s = _stream_handle(Q, stream)
     work, wanted = None, 0
