@@ -332,3 +332,22 @@ def test_queries_that_are_no_numbers_among_many_heads(lib, d):
             assert not torch.isfinite(dK[b, h, i]).any()
         for g, w, e, c, name in zip((dQ, dK, dV), want, bounds, (clean[0], clean[1], clean[1]), ("dQ", "dK", "dV")):
             ref.within(g[c], w[c], e[c], name)
+
+
+def test_rows_far_apart(lib):
+    """Rows of keys, values and queries 36 MB apart, more than 2^32 bytes from the first to the last: offsets past 32 bits, and strides that the
+    copies of whole tiles do not take."""
+    N, M, d, step = 100, 130, 64, 18 << 20
+    pool = torch.empty(step * M, dtype=torch.bfloat16, device=DEV)
+    at = lambda offset, rows: pool.as_strided((1, 1, rows, d), (0, 0, step, 1), offset)  # noqa: E731
+    Q, K, V, dO = (at(i * 4096, M if i in (1, 2) else N) for i in range(4))
+    for i, t in enumerate((Q, K, V, dO)):
+        t.copy_(normal(t.shape, 71 + i))
+    own = [t.clone(memory_format=torch.contiguous_format) for t in (Q, K, V, dO)]
+    want, lse = lib.recurrence_attention_window(*own[:3], 50, 3)
+    grads = lib.recurrence_attention_window_grad(*own[:3], want, lse, own[3], 50, 3)
+    got, glse = lib.recurrence_attention_window(Q, K, V, 50, 3)
+    assert torch.equal(got, want) and torch.equal(glse, lse)
+    for g, w in zip(lib.recurrence_attention_window_grad(Q, K, V, want, lse, dO, 50, 3), grads):
+        assert torch.equal(g, w)
+    ref.within(got, *(lambda f: (f[0], f[2]))(ref.forward(*own[:3], 50, 3)), "O")
