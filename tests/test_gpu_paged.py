@@ -359,3 +359,32 @@ def test_few_rows_with_runs_beside_many_without(lib):
     lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, batch.lens, starts, window=window, sinks=sinks, out=out)
     batch.check(out, window, sinks, only=range(1, 9))
     assert bool(out[:1].isnan().all())
+
+
+@pytest.mark.parametrize("case", [
+    ([1] * 70 + [3], [50 + i for i in range(70)] + [900], 8, 8, 64, 16, None, 0),
+    ([129] * 3 + [1] * 80 + [40], [129 + i for i in range(3)] + [1000 + i for i in range(80)] + [2222], 16, 2, 64, 32, None, 0),
+    ([17] * 66, [700 + 3 * i for i in range(66)], 16, 1, 128, 16, None, 0), ([300, 2], [6000, 9000], 64, 8, 128, 16, None, 0),
+    ([2, 40], [600, 50], 12, 3, 128, 65536, None, 0), ([1, 5, 300, 1], [3000, 5, 700, 1], 4, 2, 128, 4096, 100, 7),
+], ids=lambda c: f"{len(c[0])} sequences, page {c[5]}")
+def test_many_sequences_and_large_pages(lib, case):
+    test_against_the_definition(lib, case, False)
+
+
+def test_a_captured_step_whose_lengths_grow(lib):
+    """How many runs there are is chosen anew in every replay."""
+    batch = Batch([260, 1, 1], [5000, 4000, 700], 8, 2, 128, 16, 31)
+    lens = batch.lens.clone()
+    step = lambda: lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, lens, batch.starts)  # noqa: E731
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for lengths in ([300, 20, 4], [2000, 4000, 1], [5000, 1500, 700], [261, 1, 700], [5000, 4000, 700]):
+        lens.copy_(whole(lengths))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = captured.clone()
+        assert torch.equal(got, step())
+    batch.check(got, None, 0)
