@@ -7,7 +7,7 @@
 // see them for dK and dV (four); P is taken again in the second.  Seven products for the five of the formulas, against the 4 bytes per
 // pair that P and dS would cost in memory, written and read: about the time of the two products, and room that grows with N M.
 // Bounded by matrix and vector work at the clock that the power limit leaves (2.05 GHz): 4 x 16 heads x 4096 x 128, causal, dQ 362 us, dK and
-// dV 512, 1.1 PFLOP/s of products; 2 x 32/8 heads, window 1024, 200 and 312.
+// dV 512, 1.1 PFLOP/s of products; 2 x 32/8 heads, window 1024, 200 and 295.
 //
 // Rows (resp. keys) stay in MFMA operand registers, as in cyc_window.hip, and the other side streams through LDS in tiles that are read
 // in two ways: row by row (16 bytes of a row per lane) for the products along d, transposed for those along rows or keys.  The
@@ -421,11 +421,11 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     const uint32_t lds_base = (uint32_t)(uintptr_t)lds;
     const int l = threadIdx.x & 63, lq = l & 15, g = l >> 4, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int mark = block * 4;
-    // the short runs of the first tiles before all others
-    const int pairs = p.batch * p.kv_heads, in_first = runs.first * runs.first_runs, sinks_end = pairs * in_first;
-    const bool early = block < sinks_end;
-    const Place at(early ? block : block - sinks_end, pairs, early ? in_first : runs.per_pair() - in_first);
-    const int pair = at.pair, slot = at.unit + (early ? 0 : in_first);
+    // the short runs of the first tiles after all others, beside the last of which they find places
+    const int pairs = p.batch * p.kv_heads, in_first = runs.first * runs.first_runs, of_others = pairs * (runs.per_pair() - in_first);
+    const bool is_first = block >= of_others;
+    const Place at(is_first ? block - of_others : block, pairs, is_first ? in_first : runs.per_pair() - in_first);
+    const int pair = at.pair, slot = at.unit + (is_first ? 0 : in_first);
     const int tile = __builtin_amdgcn_readfirstlane(slot < in_first ? slot / runs.first_runs : runs.first + (slot - in_first) / runs.runs);
     const int run = slot - runs.slot(tile), nruns = runs.runs_of(tile);
     const int64_t b = __builtin_amdgcn_readfirstlane(pair / p.kv_heads);
@@ -813,9 +813,9 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, c
 }
 
 // How the rows of a tile of keys are cut.  The chip takes 512 workgroups at a time, which count in rounds: 496 and 64 of the same length last
-// twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so, 312 now).  The tiles of sinks, whose rows are all that
-// follow, go first in many short runs, which fill what the others leave over; those are cut where that makes fewer or shorter
-// rounds, at a cost: three steps of 32 rows to start a run, the partial sums, written and read, and a launch.
+// twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so).  The tiles of sinks, whose rows are all that
+// follow, go last in many short runs, which fill what the others leave over (the whole gradient 511 us with them first, 481 so); the others are cut where
+// that makes fewer or shorter rounds, at a cost: three steps of 32 rows to start a run, the partial sums, written and read, and a launch.
 constexpr int64_t MOST_PART = 128 << 20;
 
 Runs choose_runs(const WindowProblem &p)
