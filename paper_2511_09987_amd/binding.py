@@ -484,6 +484,8 @@ def _elsewhere(call, tensor, stream, *args):
     """call(*args, stream) with the tensor's device as the current one and `stream`, where one is given, as its current stream: what is
     allocated inside comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it."""
     import torch
+    if getattr(stream, "device", tensor.device) != tensor.device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors are on {tensor.device}")
     with torch.cuda.device(tensor.device):
         if isinstance(stream, torch.cuda.Stream) and stream.device == tensor.device:
             with torch.cuda.stream(stream):
@@ -675,7 +677,7 @@ def cache_append(K, V, K_cache, V_cache, table, lengths, starts, stream=None):
     page table[b, j // page].  Tokens without a place (no sequence, key, or page) are not written.  Allocates nothing.
     """
     import torch
-    if K.is_cuda and K.get_device() != torch.cuda.current_device():
+    if K.is_cuda and (stream is not None or K.get_device() != torch.cuda.current_device()):
         return _elsewhere(_append, K, stream, K, V, K_cache, V_cache, table, lengths, starts)
     return _append(K, V, K_cache, V_cache, table, lengths, starts, stream)
 

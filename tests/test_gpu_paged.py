@@ -388,3 +388,17 @@ def test_a_captured_step_whose_lengths_grow(lib):
         got = captured.clone()
         assert torch.equal(got, step())
     batch.check(got, None, 0)
+
+
+def test_a_stream_of_another_device_is_refused(lib):
+    from types import SimpleNamespace
+    batch, other = Batch([1], [40], 2, 2, 64, 16, 9), SimpleNamespace(device=torch.device("cuda", 1), cuda_stream=0)
+    K = batch.keys[0][0].transpose(0, 1)[-1:].contiguous()
+    Q = batch.Q[None].transpose(1, 2)
+    lse = torch.zeros(Q.shape[:3], device=DEV)
+    for call in (lambda: lib.recurrence_attention_paged(batch.Q, *batch.arguments(), stream=other), lambda: lib.cache_append(K, K, *batch.arguments(), stream=other),
+                 lambda: lib.recurrence_attention_window(Q, Q, Q, stream=other), lambda: lib.recurrence_attention_window_grad(Q, Q, Q, Q, lse, Q, stream=other)):
+        with pytest.raises(ValueError, match="the stream is on cuda:1"):
+            call()
+    lib.cache_append(K, K, *batch.arguments(), stream=torch.cuda.Stream(DEV))
+    torch.cuda.synchronize()
