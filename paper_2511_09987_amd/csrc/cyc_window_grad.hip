@@ -433,7 +433,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     const int group = p.group, N = p.N, M = p.M, window = p.window, sinks = p.sinks;
 
     // ---- the queries that see any of the keys k_first .. k_last, as tiles (head, 32 queries): first those whose queries all see all keys of the
-    // workgroup, head by head, then the others; this run's share of them
+    // workgroup, head by head, then the others; this run's share of them.  (The same share with CAREFUL, which repeats single runs beside others.)
     const int shift = M - N, k_first = tile * KEYS, k_last = (M - k_first < KEYS ? M : k_first + KEYS) - 1;
     const int i_first = k_first > shift ? k_first - shift : 0;
     const int64_t reach = (int64_t)k_last + window - 1 - shift;
@@ -443,7 +443,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
     const int64_t all_reach = (int64_t)k_first + window - TILE - shift;                              // the last tile's first query
     const int all_to = k_first + KEYS <= sinks || all_reach >= N ? N / TILE : all_reach < 0 ? 0 : min((int)(all_reach / TILE) + 1, N / TILE);
     const int w_first = all_from > t_first ? all_from : t_first;
-    const int whole = CAREFUL || k_first + KEYS > M || all_to <= w_first ? 0 : all_to - w_first;     // of a head
+    const int whole = k_first + KEYS > M || all_to <= w_first ? 0 : all_to - w_first;     // of a head
     const int others = per_head - whole, all_tiles = per_head * group, whole_tiles = whole * group;
     const int o_first = whole > 0 && w_first == t_first ? w_first + whole : t_first;
     const int u_first = __builtin_amdgcn_readfirstlane((int)((int64_t)all_tiles * run / nruns));
@@ -674,7 +674,7 @@ __device__ __forceinline__ void keys_of_block(const WindowProblem &p, const Runs
         ++u;
     };
     if (u_first < u_last) issue(u_first);
-    while (u < u_last && u < whole_tiles) {
+    while (!CAREFUL && u < u_last && u < whole_tiles) {
         arrive();
         touched = true;
         stream_tile(std::false_type{}, lds + ((u - u_first) & 1) * STAGE);

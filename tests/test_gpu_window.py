@@ -351,3 +351,38 @@ def test_rows_far_apart(lib):
     for g, w in zip(lib.recurrence_attention_window_grad(Q, K, V, want, lse, dO, 50, 3), grads):
         assert torch.equal(g, w)
     ref.within(got, *(lambda f: (f[0], f[2]))(ref.forward(*own[:3], 50, 3)), "O")
+
+
+# batch, heads, kv_heads, N, M, d, window, sinks: calls whose keys have their rows cut into runs, and tiles of queries that all see all keys of a tile
+CUT_CASES = [(1, 2, 2, 1024, 1024, 64, None, 0), (1, 2, 1, 1024, 1024, 128, 300, 0), (1, 2, 2, 2000, 2000, 64, 300, 4), (1, 2, 1, 1500, 1500, 128, 400, 200)]
+
+
+@pytest.mark.parametrize("case", CUT_CASES, ids=str)
+def test_no_numbers_beside_runs_of_rows(lib, case):
+    """One query, dO, key or value without numbers where the rows of a tile of keys are cut into runs: gradients that meet it in no visible pair
+    stay what they are, those that do are no numbers.  A query is in a masked tile for the keys around it and in a whole one for those before."""
+    batch, heads, kv, N, M, d, window, sinks = case
+    Q, K, V = operands(batch, heads, kv, N, M, d, 61)
+    dO = normal(Q.shape, 62)
+    O, lse, _, _ = ref.forward(Q, K, V, window, sinks)
+    O, lse = O.to(torch.bfloat16), lse.float()
+    want, bounds = ref.gradient(Q, K, V, O, lse, dO, window, sinks)
+    seen = ref.visible(N, M, window, sinks, DEV)
+    none = torch.zeros(M, dtype=torch.bool, device=DEV)
+    for at in (300, 655, 1000):
+        for which in ("Q", "dO", "K", "V"):
+            for bad in (math.nan, math.inf):
+                x = {"Q": Q, "dO": dO, "K": K, "V": V}
+                x[which] = x[which].clone()
+                x[which][:, :, at] = bad
+                got = lib.recurrence_attention_window_grad(x["Q"], x["K"], x["V"], O, lse, x["dO"], window, sinks)
+                if which in ("Q", "dO"):
+                    queries, keys = none[:N].clone(), seen[at]
+                    queries[at] = True
+                else:
+                    queries, keys = seen[:, at], none.clone()
+                    keys[at] = True
+                spoilt = queries, keys, keys if which != "V" else none             # (dV does not depend on V)
+                for name, g, w, b, off in zip(("dQ", "dK", "dV"), got, want, bounds, spoilt):
+                    ref.within(g[:, :, ~off], w[:, :, ~off], b[:, :, ~off], f"{name}, {which} {at} {bad}")
+                    assert not torch.isfinite(g[:, :, off]).any(), f"{name}, {which} {at} {bad}"
