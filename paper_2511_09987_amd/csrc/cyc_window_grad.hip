@@ -826,7 +826,7 @@ Runs choose_runs(const WindowProblem &p)
     const int64_t step = p.d == 128 ? 1500 : 900;                     // nanoseconds, two workgroups on a compute unit
     const bool cut = steps < all_steps;                               // else every tile's rows are those that follow
     int64_t early = 0, early_length = 0;                              // runs of sinks
-    if (cut && p.sinks > 0) {
+    if (cut && p.sinks > 0 && best.tiles > 0) {
         best.first = (int)std::min<int64_t>(best.tiles, ((int64_t)std::min(p.sinks, p.M) + KEYS - 1) / KEYS);
         best.first_runs = (int)std::max<int64_t>(1, std::min<int64_t>({(all_steps + 15) / 16, 1024 / (pairs * best.first), MOST_PART / 2 / (part * best.first), MOST_RUNS}));
         early = pairs * best.first * best.first_runs;

@@ -386,3 +386,13 @@ def test_no_numbers_beside_runs_of_rows(lib, case):
                 for name, g, w, b, off in zip(("dQ", "dK", "dV"), got, want, bounds, spoilt):
                     ref.within(g[:, :, ~off], w[:, :, ~off], b[:, :, ~off], f"{name}, {which} {at} {bad}")
                     assert not torch.isfinite(g[:, :, off]).any(), f"{name}, {which} {at} {bad}"
+
+
+@pytest.mark.parametrize("d", (64, 128))
+def test_many_queries_without_keys(lib, d):
+    """Far more queries than the window is wide, and no keys: outputs and gradients of zeros."""
+    Q, K, V = operands(1, 4, 2, 500, 0, d, 71)
+    O, lse = lib.recurrence_attention_window(Q, K, V, 16, 4)
+    assert not O.any() and lse.isneginf().all()
+    dQ, dK, dV = lib.recurrence_attention_window_grad(Q, K, V, O, lse, normal(Q.shape, 72), 16, 4, dQ=torch.full_like(Q, 7.0))
+    assert not dQ.any() and dK.shape == K.shape and dV.shape == V.shape

@@ -177,3 +177,12 @@ def test_gradient_of_keys_without_queries(pkg):
     assert grad(pkg, heads=0, dk=0) == NULL and grad(pkg, heads=0, dv=DK) == ALIAS and grad(pkg, heads=0, size=16) == WORKSPACE
     assert grad(pkg, heads=0, M=0, q=0, k=0, v=0, o=0, lse=0, do=0, dq=0, dk=0, dv=0) == 0
     assert grad(pkg, batch=0, kv=1 << 40, heads=1 << 40, M=1 << 29) == 0
+
+
+@pytest.mark.parametrize("N,window,sinks", [(500, 16, 4), (1 << 20, 1, 1), (500, 0, 0), (500, 16, 0), (1, 16, 4)])
+def test_gradient_of_queries_without_keys(pkg, N, window, sinks):
+    """No keys: room for the statistics of the queries alone, 8 bytes for each row of whole tiles of 32, whatever the mask."""
+    rows = -(-N // 32) * 32
+    for d in (64, 128):
+        assert pkg.cyc_attention_window_grad_workspace(1, 4, 2, N, 0, d, window, sinks) == -(-4 * rows * 8 // 256) * 256
+    assert grad(pkg, N=500, M=0, w=window, sinks=sinks, size=16) == WORKSPACE     # (a million queries would meet the next operand)
