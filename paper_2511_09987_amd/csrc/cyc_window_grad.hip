@@ -816,6 +816,7 @@ __global__ __launch_bounds__(256) void grad_join_kernel(const WindowProblem p, c
 // twice as long as 496 (2 x 8 key heads x 4096 x 128, window 1024, sinks 4: 378 us so).  The tiles of sinks, whose rows are all that
 // follow, go last in many short runs, which fill what the others leave over (the whole gradient 511 us with them first, 481 so); the others are cut where
 // that makes fewer or shorter rounds, at a cost: three steps of 32 rows to start a run, the partial sums, written and read, and a launch.
+// The partial sums of the sinks' tiles, and those of the others, take 64 MB at most.
 constexpr int64_t MOST_PART = 128 << 20;
 
 Runs choose_runs(const WindowProblem &p)
@@ -834,7 +835,10 @@ Runs choose_runs(const WindowProblem &p)
     }
     const int64_t others = pairs * (best.tiles - best.first), mean = cut ? steps : (steps + 1) / 2;
     int64_t best_cost = INT64_MAX;
-    for (int64_t r = 1; r == 1 || (r <= 32 && steps / r >= 8 && part * (best.tiles - best.first) * r <= MOST_PART / 2); ++r) {
+    // (tiles of sinks have at least as many runs as the others: grad_join_kernel goes through all tiles or those alone)
+    auto runs_of_first = [&](int64_t r) { return best.first == 0 ? 0 : std::max<int64_t>(best.first_runs, r); };
+    auto fits = [&](int64_t r) { return part * (best.tiles - best.first) * r <= MOST_PART / 2 && part * best.first * runs_of_first(r) <= MOST_PART / 2; };
+    for (int64_t r = 1; r == 1 || (r <= 32 && others > 0 && steps / r >= 8 && fits(r)); ++r) {
         const int64_t n = others * r, length = (mean + r - 1) / r + 3, longest = (steps + r - 1) / r + 3, work = (early * early_length + n * length) / 512;
         int64_t time;                                                 // in steps
         if (!cut) time = std::max(work, longest);                     // (rows of very different numbers even out)
@@ -842,14 +846,13 @@ Runs choose_runs(const WindowProblem &p)
         else if (n <= 512) time = early_length + length;
         else time = std::max(early_length + 2 * length, work + length / 2);
         int64_t cost = time * step;
-        if (r > 1) cost += 6000 + part * (best.tiles - best.first) * r / 2000;
+        if (r > 1) cost += 6000 + part * ((best.tiles - best.first) * r + best.first * (runs_of_first(r) - runs_of_first(1))) / 2000;
         if (cost < best_cost) {
             best_cost = cost;
             best.runs = (int)r;
         }
     }
-    best.first_runs = std::max(best.first_runs, best.runs);
-    if (best.first == 0) best.first_runs = best.runs;
+    best.first_runs = best.first == 0 ? best.runs : (int)runs_of_first(best.runs);
     return best;
 }
 

@@ -396,3 +396,8 @@ def test_many_queries_without_keys(lib, d):
     assert not O.any() and lse.isneginf().all()
     dQ, dK, dV = lib.recurrence_attention_window_grad(Q, K, V, O, lse, normal(Q.shape, 72), 16, 4, dQ=torch.full_like(Q, 7.0))
     assert not dQ.any() and dK.shape == K.shape and dV.shape == V.shape
+
+
+@pytest.mark.parametrize("case", [(1, 2, 1, 1500, 1500, 128, 400, 1400), (1, 2, 2, 2000, 2000, 64, 300, 2000), (2, 12, 2, 700, 600, 64, 128, 500)], ids=str)
+def test_gradients_of_almost_all_keys_as_sinks(lib, case):
+    test_gradient(lib, case)

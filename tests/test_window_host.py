@@ -186,3 +186,15 @@ def test_gradient_of_queries_without_keys(pkg, N, window, sinks):
     for d in (64, 128):
         assert pkg.cyc_attention_window_grad_workspace(1, 4, 2, N, 0, d, window, sinks) == -(-4 * rows * 8 // 256) * 256
     assert grad(pkg, N=500, M=0, w=window, sinks=sinks, size=16) == WORKSPACE     # (a million queries would meet the next operand)
+
+
+@pytest.mark.parametrize("case", [(4, 16, 16, 8192, 8192, 128, 4096, 8191), (4, 16, 16, 8192, 8192, 128, 4096, 8000), (8, 256, 128, 4096, 3, 64, 2690, 511),
+                                  (2, 64, 8, 8192, 8192, 64, 700, 5000), (1, 32, 8, 30000, 30000, 128, 1024, 29000)], ids=str)
+def test_partial_sums_of_many_sinks_are_bounded(pkg, case):
+    """8 bytes for each row, 64 MB at most for each of the partial sums of rows, of keys with sinks and of other keys, and 32 bytes for each
+    workgroup, of which there are at most 256 for each tile of 128 keys."""
+    batch, heads, kv, N, M, d, window, sinks = case
+    rows, tiles = -(-N // 32) * 32, -(-M // 128)
+    wanted = pkg.cyc_attention_window_grad_workspace(*case)
+    assert 0 < wanted <= batch * heads * rows * 8 + 3 * (64 << 20) + batch * kv * tiles * 256 * 32
+    assert wanted <= 2 * pkg.cyc_attention_window_grad_workspace(batch, heads, kv, N, M, d, window, 0) + (192 << 20)
