@@ -50,6 +50,23 @@ constexpr int LEAST_TILES = 8;           // of a run of few rows: what pays for 
 
 enum Addressing { DENSE, PAGED_SHORT, PAGED_LONG };
 
+// Sequence b's new tokens, those that lie within the call's whatever starts and lengths hold, and its keys: none where `bad`, and the rows are
+// NaN.  What a workgroup writes and what joins it go by these numbers alone.
+struct Sequence {
+    int first, N, M;
+    bool bad;
+    __device__ __forceinline__ Sequence(const TileProblem &p, int b)
+    {
+        const int start = p.starts[b], end = p.starts[b + 1];
+        M = p.lengths[b];
+        bad = start < 0 || end > p.tokens || end < start || M < 0 || M > ((int64_t)p.max_pages << p.page_shift);
+        first = start < 0 ? 0 : start > p.tokens ? p.tokens : start;
+        N = (end < first ? first : end > p.tokens ? p.tokens : end) - first;
+        bad |= N > p.max_new;
+        if (bad) M = 0;
+    }
+};
+
 // What a workgroup finds out about the sequences of its call, 64 at a time, a lane for each.
 __device__ __forceinline__ int wave_most(int x)
 {
@@ -200,14 +217,11 @@ __global__ __launch_bounds__(NWAVE * 64, 2) void tile_kernel(const TileProblem p
             b = rows.seq;
             tile = rows.tile;
         }
-        int start = p.starts[b], end = p.starts[b + 1];
-        M = p.lengths[b];
-        bad = start < 0 || end > p.tokens || end < start || M < 0 || M > ((int64_t)p.max_pages << p.page_shift);
-        first = start < 0 ? 0 : start > p.tokens ? p.tokens : start;
-        end = end < first ? first : end > p.tokens ? p.tokens : end;
-        N = end - first;
-        if (N > p.max_new) bad = true;
-        if (bad) M = 0;
+        const Sequence of(p, b);
+        first = of.first;
+        N = of.N;
+        M = of.M;
+        bad = of.bad;
         if (N == 0) return;
         if constexpr (A == PAGED_SHORT) {
             // longer sequences have a launch of their own, unless the caller had announced that there are none
@@ -606,39 +620,35 @@ template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(
     int64_t b = 0, row, at;                                           // problem; row of O; row among the parts
     bool few;
     if constexpr (PAGED) {
-        int seq, start, end;
+        int seq, r = 0;
         if (by_slot) {
             at = (int64_t)blockIdx.x * PER + threadIdx.x / (D / 4);
             if (at >= shorts.rows) return;
-            const int unit = (int)(at / SHORT_ROWS), r = (int)(at % SHORT_ROWS);
+            const int unit = (int)(at / SHORT_ROWS);
+            r = (int)(at % SHORT_ROWS);
             seq = unit / p.kv_heads;
-            start = p.starts[seq], end = p.starts[seq + 1];
-            position = p.lengths[seq] - end;
-            if (start < 0 || end > p.tokens || end - start > p.max_new || p.lengths[seq] < 0) position = 0;
-            start = start < 0 ? 0 : start > p.tokens ? p.tokens : start;
-            end = end < start ? start : end > p.tokens ? p.tokens : end;
-            if (r >= (end - start) * p.group || (int64_t)(end - start) * p.group > p.short_rows) return;
-            i = start + r / p.group;
             h = (unit - seq * p.kv_heads) * p.group + r % p.group;
-            row = (int64_t)i * heads + h;
-            few = true;
-            position += i;
+            i = 0;
         } else {
             // a workgroup's rows are of one token, whose sequence it looks up once
             const int chunks = (heads + PER - 1) / PER;
             i = blockIdx.x / chunks;
             h = (blockIdx.x - i * chunks) * PER + threadIdx.x / (D / 4);
             if (h >= heads) return;
-            at = row = (int64_t)i * heads + h;
-            seq = sequence_of(p.starts, p.batch, i), start = p.starts[seq], end = p.starts[seq + 1];
-            const int n = end - start;
-            if (i < start || i >= end) return;
-            few = (int64_t)n * p.group <= p.short_rows;
-            if (!few && longs.splits == 0) return;                    // (no launch for it: its rows are NaN already)
-            if (few) at = ((int64_t)seq * p.kv_heads + h / p.group) * SHORT_ROWS + (i - start) * p.group + h % p.group;
-            position = p.lengths[seq] - end + i;
-            if (start < 0 || end > p.tokens || n > p.max_new || p.lengths[seq] < 0) position = 0;
+            seq = sequence_of(p.starts, p.batch, i);
         }
+        const Sequence of(p, seq);
+        few = (int64_t)of.N * p.group <= p.short_rows;
+        if (by_slot) {
+            if (r >= of.N * p.group || !few) return;
+            i = of.first + r / p.group;
+        } else {
+            if (i < of.first || i >= of.first + of.N) return;
+            if (!few && longs.splits == 0) return;                    // (no launch for it: its rows are NaN already)
+        }
+        row = (int64_t)i * heads + h;
+        if (!by_slot) at = few ? ((int64_t)seq * p.kv_heads + h / p.group) * SHORT_ROWS + (i - of.first) * p.group + h % p.group : row;
+        position = of.bad ? 0 : of.M - of.N + i - of.first;
     } else {
         at = row = (int64_t)blockIdx.x * PER + threadIdx.x / (D / 4);
         if (row >= p.rows) return;

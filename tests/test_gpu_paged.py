@@ -402,3 +402,17 @@ def test_a_stream_of_another_device_is_refused(lib):
             call()
     lib.cache_append(K, K, *batch.arguments(), stream=torch.cuda.Stream(DEV))
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("new,lengths,heads,kv", [([1, 1, 1], [1500, 900, 2100], 8, 2), ([2, 5, 3], [1500, 900, 2100], 4, 4), ([40, 1, 60], [1500, 900, 2100], 8, 2)])
+def test_starts_far_outside_the_tokens(lib, new, lengths, heads, kv):
+    """Sequences whose runs are joined: the one with the wrong start has NaN in its rows, the others what they had."""
+    batch = Batch(new, lengths, heads, kv, 64, 16, 41)
+    for max_new in (None, max(new)):
+        for at, value, wrong in ((0, -1, 0), (0, -3, 0), (0, -2 ** 31, 0), (3, batch.rows[-1] + 1, 2), (3, 2 ** 31 - 1, 2)):
+            starts = batch.starts.clone()
+            starts[at] = value
+            out = torch.full(batch.Q.shape, 7.0, dtype=torch.bfloat16, device=DEV)
+            lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, batch.lens, starts, max_new=max_new, out=out)
+            batch.check(out, None, 0, only=[b for b in range(3) if b != wrong])
+            assert bool(out[batch.rows[wrong]:batch.rows[wrong + 1]].isnan().all()), (max_new, at, value)
