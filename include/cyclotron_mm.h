@@ -345,7 +345,7 @@ typedef struct {
  * dense.  lengths, starts and table are read on the device.  A token that belongs to no sequence, stands before key 0 or behind
  * max_pages, or whose page is not in [0, pages), is not written; starts outside [0, tokens] leave their sequence unwritten.  Two tokens
  * of one call that the table sends to the same place leave either.
- * tokens or seqs == 0: CYC_OK, nothing done.  Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE, CYC_ERR_ALIAS (the cache
+ * tokens or seqs == 0: CYC_OK, nothing done.  Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE (also K of 64 GiB and more), CYC_ERR_ALIAS (the cache
  * overlaps K, V, table, lengths or starts, or its keys and values have memory in common), CYC_ERR_LAUNCH. */
 int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64_t tokens, const int64_t *strides, void *stream);
 

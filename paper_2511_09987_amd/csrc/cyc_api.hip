@@ -9,7 +9,6 @@
 #include <atomic>
 #include <algorithm>
 #include <climits>
-#include <cstdlib>
 #include <utility>
 
 namespace {
@@ -645,7 +644,7 @@ int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64
     int64_t t;
     if (!cache_extents(c, tokens, &shift) || !mul_ok(tokens, c.kv_heads * c.d, &t) || !token_strides(strides, K, V, tokens, c.kv_heads, c.d, false, x))
         return CYC_ERR_SHAPE;
-    if (t / 8 >= ((int64_t)1 << 38)) return CYC_ERR_SHAPE;        // (a grid of 2^31 workgroups of 128 chunks)
+    if (t / 8 > (int64_t)cyc::MOST_THREADS - 255) return CYC_ERR_SHAPE;       // (a thread for 16 bytes, workgroups of 256)
     if (tokens == 0 || c.seqs == 0) return CYC_OK;
     if (!K || !V || !c.K || !c.V || !c.table || !c.lengths || !c.starts) return CYC_ERR_NULL;
     if (((uintptr_t)K | (uintptr_t)V | (uintptr_t)c.K | (uintptr_t)c.V) & 15 || ((uintptr_t)c.table | (uintptr_t)c.lengths | (uintptr_t)c.starts) & 3)

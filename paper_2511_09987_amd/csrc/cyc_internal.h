@@ -11,12 +11,15 @@
 
 namespace cyc {
 
+constexpr uint64_t MOST_THREADS = UINT32_MAX;   // along one dimension of a launch
+
 // Enqueue `kernel` and return the status of this launch itself: unlike the triple-chevron form followed by
 // hipGetLastError(), this neither consumes nor reports an error that an earlier call of the application left behind.
 template <typename... KArgs, typename... Args>
 inline hipError_t launch_kernel(void (*kernel)(KArgs...), dim3 grid, dim3 block, hipStream_t s, Args &&...args)
 {
     static_assert(sizeof...(KArgs) == sizeof...(Args), "argument count does not match the kernel's signature");
+    if ((uint64_t)grid.x * block.x > MOST_THREADS) return hipErrorInvalidConfiguration;
     std::tuple<std::remove_cv_t<KArgs>...> vals(static_cast<std::remove_cv_t<KArgs>>(args)...);
     void *ptrs[sizeof...(KArgs)];
     std::apply([&](auto &...v) { int i = 0; ((ptrs[i++] = (void *)&v), ...); }, vals);

@@ -416,3 +416,15 @@ def test_starts_far_outside_the_tokens(lib, new, lengths, heads, kv):
             lib.recurrence_attention_paged(batch.Q, *batch.caches, batch.table, batch.lens, starts, max_new=max_new, out=out)
             batch.check(out, None, 0, only=[b for b in range(3) if b != wrong])
             assert bool(out[batch.rows[wrong]:batch.rows[wrong + 1]].isnan().all()), (max_new, at, value)
+
+
+def test_more_sequences_than_a_launch_takes(lib):
+    """2^22 sequences x 16 key heads x 64 threads are 2^32, one more than a launch has: refused, and nothing is written."""
+    seqs, cache = 1 << 22, torch.zeros((1, 16, 16, 64), dtype=torch.bfloat16, device=DEV)
+    starts = torch.zeros(seqs + 1, dtype=torch.int32, device=DEV)
+    starts[-1] = 1
+    out = torch.full((1, 16, 64), 7.0, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(lib.CycError, match="LAUNCH"):
+        lib.recurrence_attention_paged(torch.zeros_like(out), cache, cache, starts[:-1].view(-1, 1), starts[:-1], starts, max_new=1, out=out)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())

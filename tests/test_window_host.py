@@ -198,3 +198,12 @@ def test_partial_sums_of_many_sinks_are_bounded(pkg, case):
     wanted = pkg.cyc_attention_window_grad_workspace(*case)
     assert 0 < wanted <= batch * heads * rows * 8 + 3 * (64 << 20) + batch * kv * tiles * 256 * 32
     assert wanted <= 2 * pkg.cyc_attention_window_grad_workspace(batch, heads, kv, N, M, d, window, 0) + (192 << 20)
+
+
+def test_the_largest_append(pkg):
+    """One launch has 2^32 - 1 threads in workgroups of 256, and a thread moves eight elements of K: 2^29 tokens of 64 are too many, 32 fewer are
+    not (and meet the check of the pointers that follows)."""
+    c, f = cache(pkg, kv_heads=1), pkg.cyc_cache_append
+    assert f(0, 0, c, 1 << 29, None) == SHAPE
+    assert f(0, 0, c, (1 << 29) - 32, None) == NULL
+    assert f(0, 0, cache(pkg), 1 << 28, None) == SHAPE and f(0, 0, cache(pkg), (1 << 28) - 16, None) == NULL
