@@ -1,6 +1,7 @@
 """Compile the HIP sources under csrc/ into paper_2511_09987_amd/libcyclotron_mm.so (gfx950 only)."""
 import glob
 import os
+import re
 import subprocess
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -26,9 +27,14 @@ def sources():
 
 
 def reads_lds_from_asm(src: str) -> bool:
-    """Does this source issue LDS reads from inline asm (their registers are valid only after a later wait)?"""
+    """Does this source, or a header of csrc that it includes, issue LDS reads from inline asm (their registers are valid only after
+    a later wait)?"""
     with open(src) as f:
-        return 'asm volatile("ds_read' in f.read()
+        text = f.read()
+    if re.search(r'"[^"\n]*\bds_read', text):
+        return True
+    headers = (os.path.join(CSRC, name) for name in re.findall(r'#include "([^"]+)"', text))
+    return any(os.path.exists(header) and reads_lds_from_asm(header) for header in headers)
 
 
 def check_async_reads(src: str) -> None:
