@@ -482,15 +482,18 @@ def cyc_recurrence_attention_paged(Q: int, cache: cyc_cache, O: int, tokens: int
 
 def _elsewhere(call, tensor, stream, *args):
     """call(*args, stream) with the tensor's device as the current one and `stream`, where one is given, as its current stream: what is
-    allocated inside comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it."""
+    allocated inside comes from the pool of the stream that the call runs on, so that no work still pending on another stream uses it.
+    A stream of another library (any object with a handle in `cuda_stream`) has a pool too, which goes by the handle."""
     import torch
     if getattr(stream, "device", tensor.device) != tensor.device:
         raise ValueError(f"the stream is on {stream.device}, the tensors are on {tensor.device}")
     with torch.cuda.device(tensor.device):
-        if isinstance(stream, torch.cuda.Stream) and stream.device == tensor.device:
-            with torch.cuda.stream(stream):
-                return call(*args, stream)
-        return call(*args, stream)
+        if stream is None:
+            return call(*args, None)
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(stream.cuda_stream, device=tensor.device)
+        with torch.cuda.stream(stream):
+            return call(*args, stream)
 
 
 def _mask_arguments(window, sinks):
@@ -613,8 +616,8 @@ def recurrence_attention_window_grad(Q, K, V, O, lse, dO, window=None, sinks: in
     """Tensor-level convenience: (dQ, dK, dV) of recurrence_attention_window from what it returned and the gradient of O.
 
     Q, K, V, window, sinks as in the forward call, O and lse what it returned, dO like O.  Allocates the gradients (bfloat16, dense, of the
-    shapes of Q, K and V) unless given and the memory that the call needs, and forwards pointers to the C ABI on the current (or given)
-    stream.
+    shapes of Q, K and V) unless given and the memory that the call needs (torch.OutOfMemoryError where there is none), and forwards pointers to
+    the C ABI on the current (or given) stream.
     """
     import torch
     if Q.is_cuda and (stream is not None or Q.get_device() != torch.cuda.current_device()):
@@ -623,6 +626,7 @@ def recurrence_attention_window_grad(Q, K, V, O, lse, dO, window=None, sinks: in
 
 
 def _attention_window_grad(Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV, stream):
+    import torch
     q, k = _attention_shapes(Q, K)
     window, sinks = _mask_arguments(window, sinks)
     batch, heads, N, d = q
@@ -635,7 +639,7 @@ def _attention_window_grad(Q, K, V, O, lse, dO, window, sinks, dQ, dK, dV, strea
     _check_lse(lse, q[:3], device)
     s = _stream_handle(Q, stream)
     wanted = cyc_attention_window_grad_workspace(batch, heads, kv_heads, N, M, d, window, sinks)
-    work = _memory(wanted, Q, stream) if wanted else None
+    work = Q.new_empty(wanted, dtype=torch.uint8) if wanted else None        # (of the stream's pool, see _elsewhere; the call cannot do without)
     st = cyc_recurrence_attention_window_grad(Q.data_ptr(), K.data_ptr(), V.data_ptr(), O.data_ptr(), lse.data_ptr(), dO.data_ptr(), dQ.data_ptr(),
                                               dK.data_ptr(), dV.data_ptr(), batch, heads, kv_heads, N, M, d, strides, window, sinks,
                                               0 if work is None else work.data_ptr(), 0 if work is None else wanted, s)

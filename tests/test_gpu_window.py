@@ -401,3 +401,45 @@ def test_many_queries_without_keys(lib, d):
 @pytest.mark.parametrize("case", [(1, 2, 1, 1500, 1500, 128, 400, 1400), (1, 2, 2, 2000, 2000, 64, 300, 2000), (2, 12, 2, 700, 600, 64, 128, 500)], ids=str)
 def test_gradients_of_almost_all_keys_as_sinks(lib, case):
     test_gradient(lib, case)
+
+
+def test_a_stream_of_another_library(lib):
+    """Any object with a stream's handle: all calls take it, and have their memory from that stream's pool."""
+    from types import SimpleNamespace
+    side = torch.cuda.Stream()
+    other = SimpleNamespace(cuda_stream=side.cuda_stream)
+    Q, K, V = operands(1, 4, 2, 300, 2100, 64, 85)
+    dO = normal(Q.shape, 86)
+    O, lse = lib.recurrence_attention_window(Q, K, V, 700, 3)
+    grads = lib.recurrence_attention_window_grad(Q, K, V, O, lse, dO, 700, 3)
+    cache, table, count = K[0].view(2, -1, 4, 64).transpose(0, 1), torch.arange(525, dtype=torch.int32, device=DEV).view(1, -1), torch.tensor([2100], dtype=torch.int32, device=DEV)
+    starts, values = torch.tensor([0, 300], dtype=torch.int32, device=DEV), V[0].view(2, -1, 4, 64).transpose(0, 1)
+    rows = Q[0].transpose(0, 1)
+    paged = lib.recurrence_attention_paged(rows, cache, values, table, count, starts, 700, 3)
+    torch.cuda.synchronize()
+    again = lib.recurrence_attention_window(Q, K, V, 700, 3, stream=other)
+    gagain = lib.recurrence_attention_window_grad(Q, K, V, *again, dO, 700, 3, stream=other)
+    pagain = lib.recurrence_attention_paged(rows, cache, values, table, count, starts, 700, 3, stream=other)
+    keys, old = K[0].transpose(0, 1), (cache.clone(), values.clone())
+    lib.cache_append(keys.contiguous(), V[0].transpose(0, 1).contiguous(), cache, values, table, count, torch.tensor([0, 2100], dtype=torch.int32, device=DEV), stream=other)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for g, w in zip((*again, *gagain, pagain, cache, values), (O, lse, *grads, paged, *old)):
+        assert torch.equal(g, w)
+
+
+def test_a_gradient_without_memory(lib):
+    """Where the memory for partial sums is not to be had the error says so."""
+    Q, K, V = operands(1, 2, 1, 1500, 1500, 128, 87)
+    O, lse = lib.recurrence_attention_window(Q, K, V, 400, 200)
+    dQ, dK, dV = (torch.empty_like(t) for t in (Q, K, V))
+    assert lib.cyc_attention_window_grad_workspace(1, 2, 1, 1500, 1500, 128, 400, 200) > 4 << 20
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    torch.cuda.set_per_process_memory_fraction(0.0)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            lib.recurrence_attention_window_grad(Q, K, V, O, lse, O, 400, 200, dQ, dK, dV)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    lib.recurrence_attention_window_grad(Q, K, V, O, lse, O, 400, 200, dQ, dK, dV)
