@@ -294,7 +294,7 @@ int cyc_recurrence_attention_split(const void *Q, const void *K, const void *V, 
  * Q, O: device, batch x heads x N x d bfloat16.  K, V: device, batch x kv_heads x M x d bfloat16.  lse: device, batch x heads x N
  * fp32, dense, or NULL: not written.  strides (host, read before the call returns): the strides in elements of batch, head and row of
  * Q, K, V and O, twelve numbers, or NULL: each dense in the order above.  Rows of d are contiguous; strides are
- * multiples of 8 and pointers 16-byte aligned.  Inputs may have strides of 0 and overlap one another; O may not meet itself.
+ * multiples of 8 (any number for an extent of one or none, here and below) and pointers 16-byte aligned.  Inputs may have strides of 0 and overlap one another; O may not meet itself.
  * d: 64 or 128.  N, M >= 0 and (heads / kv_heads) * N below 2^30, batch * heads below 2^24; window, sinks >= 0.
  * Scores, maxima, sums and outputs are fp32 until O is rounded; the weights enter the product with V rounded to bfloat16 and
  * their sum unrounded.  What lies in keys that a query does not see never reaches it, infinities and NaN included.

@@ -526,6 +526,11 @@ def _empty_like(t):
     return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
 
 
+def _steps(t):
+    """The strides that count: those of all dimensions but the last, 0 for those of one element or none, which torch leaves open."""
+    return [s if n > 1 else 0 for n, s in zip(t.shape[:-1], t.stride())]
+
+
 def _check_rows(name, t, shape, device):
     """A bfloat16 tensor of `shape` on `device` whose rows a kernel can read 16 bytes at a time."""
     import torch
@@ -537,7 +542,7 @@ def _check_rows(name, t, shape, device):
         raise ValueError(f"shape mismatch: {name} is {tuple(t.shape)}, expected {tuple(shape)}")
     if t.get_device() != device:
         raise ValueError("all tensors must be on one device")
-    if t.stride(-1) != 1 and t.numel() or t.data_ptr() & 15 or any(s % 8 for s in t.stride()[:-1]):
+    if t.stride(-1) != 1 and t.numel() or t.data_ptr() & 15 or any([s % 8 for s in _steps(t)]):
         raise ValueError(f"{name} needs contiguous rows at multiples of 16 bytes")
 
 
@@ -652,7 +657,7 @@ def _cache(K_cache, V_cache, table, lengths, starts, name, t):
     """The tensors of a cache, checked, as the C ABI takes them, and the device of the call, that of tensor `t`."""
     import torch
     shape, strides = K_cache.shape, K_cache.stride()
-    if len(shape) != 4 or strides != V_cache.stride():
+    if len(shape) != 4 or (strides != V_cache.stride() and (V_cache.shape != shape or _steps(K_cache) != _steps(V_cache))):
         raise ValueError("K_cache and V_cache must be (pages, kv_heads, page, d) with the same strides")
     device = _device_of(name, t)
     _operands((("K_cache", K_cache, shape), ("V_cache", V_cache, shape)), device)

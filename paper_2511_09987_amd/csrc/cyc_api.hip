@@ -296,6 +296,7 @@ bool strides_ok(const Operand &x, int64_t d)
 {
     int64_t total = d, t;
     for (int i = 0; i < 3; ++i) {
+        if (x.extent[i] <= 1) continue;                  // (a stride that nothing takes)
         if (x.stride[i] < 0 || x.stride[i] % 8 || !mul_ok(x.extent[i], x.stride[i], &t)) return false;
         if ((total += t) > kMaxElems) return false;
     }

@@ -428,3 +428,18 @@ def test_more_sequences_than_a_launch_takes(lib):
         lib.recurrence_attention_paged(torch.zeros_like(out), cache, cache, starts[:-1].view(-1, 1), starts[:-1], starts, max_new=1, out=out)
     torch.cuda.synchronize()
     assert bool((out == 7.0).all())
+
+
+def test_strides_of_one_element(lib):
+    """One key head, one page, one token: the strides of such dimensions may be any, and differ between keys and values."""
+    page, d = 128, 64
+    keys, values = normal((page, d), 1), normal((page, d), 2)
+    K_cache, V_cache = torch.zeros_like(keys), torch.zeros_like(values)
+    views = K_cache.as_strided((1, 1, page, d), (3, 5, d, 1)), V_cache.as_strided((1, 1, page, d), (8, d, d, 1))
+    table, lengths = whole([[0]]), whole([100])
+    lib.cache_append(keys[:100].view(100, 1, d), values[:100].as_strided((100, 1, d), (d, 1, 1)), *views, table, lengths, whole([0, 100]))
+    assert torch.equal(K_cache[:100], keys[:100]) and torch.equal(V_cache[:100], values[:100]) and not K_cache[100:].any()
+    Q = normal((1, 6, d), 3)
+    O = lib.recurrence_attention_paged(Q.as_strided((1, 6, d), (1, d, 1)), *views, table, lengths, whole([0, 1]))
+    want, _, bound, _ = ref.forward(Q[:, :, None], keys[None, None, :100], values[None, None, :100], None, 0)
+    ref.within(O[:, :, None], want, bound)

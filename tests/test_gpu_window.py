@@ -443,3 +443,25 @@ def test_a_gradient_without_memory(lib):
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     lib.recurrence_attention_window_grad(Q, K, V, O, lse, O, 400, 200, dQ, dK, dV)
+
+
+def test_strides_of_one_element(lib):
+    """Dimensions of one element may have any stride: a single query out of (heads, d, 1), a key head out of a tensor of odd rows."""
+    batch, heads, M, d = 1, 4, 90, 64
+    Q, K, V = operands(batch, heads, 1, 1, M, d, 95)
+    odd = Q.view(batch, heads, d, 1).transpose(2, 3)                               # strides 256, 64, 1, 1
+    assert odd.stride(2) == 1
+    shared = K[0, 0].as_strided((1, 1, M, d), (7, 3, d, 1))
+    tall = torch.zeros((M, 2, d), dtype=torch.bfloat16, device=DEV)
+    tall[:, 0] = V[0, 0]
+    views = odd, shared, tall[:, :1].permute(1, 0, 2)[None]                         # (the last is not contiguous: strides are looked at)
+    want, wlse, bound, lbound = ref.forward(Q, K, V, 33, 2)
+    O, lse = lib.recurrence_attention_window(*views, 33, 2)
+    ref.within(O, want, bound, "O")
+    ref.within(lse, wlse, lbound, "lse")
+    out = torch.zeros_like(Q).view(batch, heads, d, 1).transpose(2, 3)
+    lib.recurrence_attention_window(*views, 33, 2, out=out)
+    assert torch.equal(out, O)
+    grads = lib.recurrence_attention_window_grad(*views, O, lse, odd, 33, 2, dQ=torch.zeros_like(Q).view(batch, heads, d, 1).transpose(2, 3))
+    for g, w in zip(grads, lib.recurrence_attention_window_grad(Q, K, V, O, lse, Q, 33, 2)):
+        assert torch.equal(g, w)

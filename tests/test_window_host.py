@@ -207,3 +207,14 @@ def test_the_largest_append(pkg):
     assert f(0, 0, c, 1 << 29, None) == SHAPE
     assert f(0, 0, c, (1 << 29) - 32, None) == NULL
     assert f(0, 0, cache(pkg), 1 << 28, None) == SHAPE and f(0, 0, cache(pkg), (1 << 28) - 16, None) == NULL
+
+
+def test_strides_that_nothing_takes(pkg):
+    """An extent of one element may have any stride (the check of the pointers comes after that of the strides)."""
+    odd = [7, 64, -3], [5, 1, 64], [-1, 9, 64], [3, 64, 3]                      # Q, O: four heads of one query; K, V: one head of eight keys
+    assert window(pkg, q=0, kv=1, N=1, strides=[s for x in odd for s in x]) == NULL
+    assert window(pkg, q=0, kv=1, N=2, strides=[s for x in odd for s in x]) == SHAPE
+    c = cache(pkg, pages=1, kv_heads=1, page_stride=3, head_stride=-5)
+    assert pkg.cyc_cache_append(0, O, c, 1, [3, 1, 1, 5]) == NULL and pkg.cyc_cache_append(0, O, c, 2, [3, 1, 1, 5]) == SHAPE
+    assert pkg.cyc_recurrence_attention_paged(0, c, O, 1, 4, [3, 64, 5, 64], 0, 0, 0) == NULL
+    assert pkg.cyc_recurrence_attention_paged(0, cache(pkg, pages=2, kv_heads=1, page_stride=3), O, 1, 4, None, 0, 0, 0) == SHAPE
