@@ -620,35 +620,33 @@ template <int D, bool PAGED> __global__ __launch_bounds__(256) void join_kernel(
     int64_t b = 0, row, at;                                           // problem; row of O; row among the parts
     bool few;
     if constexpr (PAGED) {
-        int seq, r = 0;
+        auto position_in = [&](const Sequence &of) { return of.bad ? 0 : of.M - of.N + i - of.first; };
         if (by_slot) {
             at = (int64_t)blockIdx.x * PER + threadIdx.x / (D / 4);
             if (at >= shorts.rows) return;
-            const int unit = (int)(at / SHORT_ROWS);
-            r = (int)(at % SHORT_ROWS);
-            seq = unit / p.kv_heads;
+            const int unit = (int)(at / SHORT_ROWS), r = (int)(at % SHORT_ROWS), seq = unit / p.kv_heads;
+            const Sequence of(p, seq);
+            if (r >= of.N * p.group || (int64_t)of.N * p.group > p.short_rows) return;
+            i = of.first + r / p.group;
             h = (unit - seq * p.kv_heads) * p.group + r % p.group;
-            i = 0;
+            row = (int64_t)i * heads + h;
+            few = true;
+            position = position_in(of);
         } else {
             // a workgroup's rows are of one token, whose sequence it looks up once
             const int chunks = (heads + PER - 1) / PER;
             i = blockIdx.x / chunks;
             h = (blockIdx.x - i * chunks) * PER + threadIdx.x / (D / 4);
             if (h >= heads) return;
-            seq = sequence_of(p.starts, p.batch, i);
-        }
-        const Sequence of(p, seq);
-        few = (int64_t)of.N * p.group <= p.short_rows;
-        if (by_slot) {
-            if (r >= of.N * p.group || !few) return;
-            i = of.first + r / p.group;
-        } else {
+            const int seq = sequence_of(p.starts, p.batch, i);
+            const Sequence of(p, seq);
             if (i < of.first || i >= of.first + of.N) return;
+            few = (int64_t)of.N * p.group <= p.short_rows;
             if (!few && longs.splits == 0) return;                    // (no launch for it: its rows are NaN already)
+            at = row = (int64_t)i * heads + h;
+            if (few) at = ((int64_t)seq * p.kv_heads + h / p.group) * SHORT_ROWS + (i - of.first) * p.group + h % p.group;
+            position = position_in(of);
         }
-        row = (int64_t)i * heads + h;
-        if (!by_slot) at = few ? ((int64_t)seq * p.kv_heads + h / p.group) * SHORT_ROWS + (i - of.first) * p.group + h % p.group : row;
-        position = of.bad ? 0 : of.M - of.N + i - of.first;
     } else {
         at = row = (int64_t)blockIdx.x * PER + threadIdx.x / (D / 4);
         if (row >= p.rows) return;
