@@ -300,7 +300,8 @@ int cyc_recurrence_attention_split(const void *Q, const void *K, const void *V, 
  * their sum unrounded.  What lies in keys that a query does not see never reaches it, infinities and NaN included.
  * workspace: as in cyc_recurrence_attention_split; cyc_attention_window_workspace says how many bytes the call wants (0: none;
  * host only, also 0 for extents that the call refuses), and with less, or NULL, the keys are not split over workgroups.
- * The same call with the same memory gives the same bits every time.  batch, heads or N == 0: CYC_OK, nothing done.
+ * The same call with the same memory gives the same bits every time.  Split keys give other bits than keys that are not: each part rounds its
+ * weights against a largest score of its own.  batch, heads or N == 0: CYC_OK, nothing done.
  * Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE (also heads no multiple of kv_heads, misaligned pointers and
  * strides, an O that meets itself), CYC_ERR_ALIAS (the memory from first to last element of O, lse or workspace overlaps that of
  * another operand), CYC_ERR_LAUNCH. */
@@ -344,7 +345,7 @@ typedef struct {
  * becomes key lengths[b] - starts[b+1] + t.  strides (host): of token and head of K and of V in elements, four numbers, or NULL:
  * dense.  lengths, starts and table are read on the device.  A token that belongs to no sequence, stands before key 0 or behind
  * max_pages, or whose page is not in [0, pages), is not written; starts outside [0, tokens] leave their sequence unwritten.  Two tokens
- * of one call that the table sends to the same place leave either.
+ * of one call that the table sends to the same place leave either there, in each 16 bytes of K and of V for itself.
  * tokens or seqs == 0: CYC_OK, nothing done.  Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE (also K of 64 GiB and more), CYC_ERR_ALIAS (the cache
  * overlaps K, V, table, lengths or starts, or its keys and values have memory in common), CYC_ERR_LAUNCH. */
 int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64_t tokens, const int64_t *strides, void *stream);
@@ -358,6 +359,7 @@ int cyc_cache_append(const void *K, const void *V, const cyc_cache *cache, int64
  * Wrong numbers on the device give NaN, not faults: a sequence of more than max_new tokens, with a length below 0 or above max_pages * page,
  * or with starts outside [0, tokens] has NaN in its rows; a table entry outside [0, pages) where a page is read puts NaN into the rows
  * that see it and may put it into other rows of that sequence.  Where starts does not ascend, rows are undefined.
+ * How keys are split depends on the lengths of all sequences of the call, and with it the last bits of each of them.
  * workspace: as for cyc_recurrence_attention_window; cyc_attention_paged_workspace says how many bytes the call wants.
  * Errors (nothing enqueued): CYC_ERR_NULL, CYC_ERR_SHAPE, CYC_ERR_ALIAS (O or workspace overlaps another operand), CYC_ERR_LAUNCH. */
 int64_t cyc_attention_paged_workspace(const cyc_cache *cache, int64_t tokens, int64_t heads, int64_t max_new, int64_t window,

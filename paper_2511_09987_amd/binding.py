@@ -583,7 +583,9 @@ def recurrence_attention_window(Q, K, V, window=None, sinks: int = 0, out=None, 
     queries are the last N of the M positions; position p sees the keys j <= p with p - j < window (None: all) or j < sinks.
     Allocates O (bfloat16, dense) and lse (float32, (batch, heads, N): the logarithms of the sums, for the gradient) unless given, and
     memory to split the keys of few queries over the chip, and forwards pointers to the C ABI on the current (or given) stream.
-    (Where that memory is not to be had the keys are not split, and the fp32 sums are added in another order.)
+    (Where that memory is not to be had the keys are not split.  Each part of split keys rounds its weights to bfloat16 against a largest score of
+    its own, so that O differs by as much as those roundings.)  Records nothing for autograd: O and lse have no graph, and
+    recurrence_attention_window_grad is what a torch.autograd.Function calls in its backward.
     """
     import torch
     if Q.is_cuda and (stream is not None or Q.get_device() != torch.cuda.current_device()):
@@ -706,7 +708,8 @@ def recurrence_attention_paged(Q, K_cache, V_cache, table, lengths, starts, wind
     Q: (tokens, heads, d), torch.bfloat16; the cache, table, lengths and starts as in cache_append, heads a multiple of kv_heads; window
     and sinks as in recurrence_attention_window.  Rows starts[b] .. starts[b+1] - 1 of Q are the last positions of sequence b.  max_new: the
     most new tokens that any sequence brings, where the caller knows it: with 1, the usual step of a decoder, only the kernel for
-    few rows is launched (a sequence that brings more has NaN in its rows then).  Allocates O (bfloat16, dense) unless given and memory to
+    few rows is launched (a sequence that brings more has NaN in its rows then).  The last bits of a row depend on how its keys are split, and that on
+    the lengths of all sequences of the call.  Records nothing for autograd.  Allocates O (bfloat16, dense) unless given and memory to
     split the keys over the chip, and forwards pointers to the C ABI on the current (or given) stream.
     """
     import torch

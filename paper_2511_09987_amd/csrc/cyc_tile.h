@@ -1,4 +1,4 @@
-// cyc_tile.h -- device helpers shared by the attention kernels: copies into LDS, reads from it that are waited for one by one,
+// cyc_tile.h -- device helpers shared by the kernels of attention with a window and its gradient: copies into LDS, reads from it that are waited for one by one,
 // reductions over the four lanes of a query, and the layout of a tile of rows.
 #pragma once
 #include "cyc_internal.h"

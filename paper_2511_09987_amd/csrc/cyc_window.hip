@@ -12,9 +12,9 @@
 // which then go to the rows that see them.  Keys that no row of the workgroup sees are not read at all: rows
 // of a tile outside [0, sinks) and the window's span are copied from a key inside.
 //
-// Many rows are bounded by matrix and vector work at the clock that the power limit leaves (32/8 heads x 8192 x 128, window 1024: 164 us,
-// 790 TFLOP/s; a tile that all rows see 1100), few rows by memory (64 sequences of 1000 to 8000 keys, 32/8 heads x 128: 218 us and 6
-// for the join, 5.4 TB/s).
+// Many rows are bounded by vector work and by what one phase of a wave waits for from another: the matrix units are busy 35 % of the time (32/8
+// heads x 8192 x 128, window 1024: 164 us, 790 TFLOP/s; a tile that all rows see 1100; with constant inputs, which draw less power, 6 % less
+// time).  Few rows are bounded by memory (64 sequences of 1000 to 8000 keys, 32/8 heads x 128: 218 us and 6 for the join, 5.4 TB/s).
 #include "cyc_window.h"
 #include "cyc_tile.h"
 

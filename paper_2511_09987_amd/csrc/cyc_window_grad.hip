@@ -6,8 +6,9 @@
 // one keeps rows (query, head) and walks their keys for dQ (three products a pair), the other keeps keys and walks the rows that
 // see them for dK and dV (four); P is taken again in the second.  Seven products for the five of the formulas, against the 4 bytes per
 // pair that P and dS would cost in memory, written and read: about the time of the two products, and room that grows with N M.
-// Bounded by matrix and vector work at the clock that the power limit leaves (2.05 GHz): 4 x 16 heads x 4096 x 128, causal, dQ 362 us, dK and
-// dV 512, 1.1 PFLOP/s of products; 2 x 32/8 heads, window 1024, 200 and 287.
+// Bounded by vector work and waits beside the products, which keep the matrix units busy 38 to 53 % of the time: 4 x 16 heads x 4096 x 128, causal,
+// 850 to 900 us in all, traced one by one dQ 363 us and dK and dV 519 at least, 1.1 PFLOP/s of products (with constant inputs, which draw less power, 12 %
+// less time); 2 x 32/8 heads, window 1024, 196 and 283.
 //
 // Rows (resp. keys) stay in MFMA operand registers, as in cyc_window.hip, and the other side streams through LDS in tiles that are read
 // in two ways: row by row (16 bytes of a row per lane) for the products along d, transposed for those along rows or keys.  The
